@@ -371,6 +371,172 @@ void jet_model_free(jet_model *model);
 /* Message of the last failed call on this thread ("" if none). */
 const char *jet_last_error(void);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Operators on device arrays: an attention cache held in 8 bits, and the
+ * adjustment of a decode step's logits. A model loaded with a JET_FLAG_QCACHE_*
+ * flag keeps its prefixes in such a cache and jet_generate_trace_rules adjusts
+ * its logits with the same kernels; these entry points offer them to programs
+ * that hold caches and logits of their own.
+ *
+ * Unlike the calls on a model, they only enqueue work on `hip_stream` (NULL:
+ * the null stream of the GPU that holds the data) and return. They allocate
+ * nothing and may be captured into a graph. Every array is device memory of
+ * one GPU (which need not be the current one), has to stay in place until the
+ * work has run, and is read and written only then. Two calls may run at the
+ * same time when neither writes what the other reads or writes; calls that
+ * overlap need workspaces of their own.
+ * What the host can see (NULL, counts, types, alignment) is refused with
+ * JET_E_INVALID before anything is enqueued. What lies in device memory cannot
+ * be refused: kernels check it against the counts given here, and a sequence
+ * or row that lies outside of them is left out (nothing is read or written
+ * for it; attention gives it zeros).
+ * ---------------------------------------------------------------------------
+ */
+
+/* Element types of rows and logits. */
+enum { JET_T_F32 = 0, JET_T_F16 = 1, JET_T_BF16 = 2 };
+
+/* 8-bit formats of a cache. A block of `block` tokens of one head shares one
+ * scale 2^e, kept as the byte e + 127 (255: the block was given a value that
+ * is not finite, and all its values are NaN). Powers of two, so that values
+ * read back exactly and a scale that grows moves the values already held by
+ * less than one step in all, however often it grows.
+ *   JET_QCACHE_INT8: value = q 2^e, q = -127 .. 127. e is the least, and not
+ *     under -60, with max|x| <= 127 2^e; q = x 2^-e rounded to nearest even.
+ *   JET_QCACHE_E4M3: value = f 2^e, f an OCP e4m3 number; max|x| <= 448 2^e. */
+enum { JET_QCACHE_INT8 = 0, JET_QCACHE_E4M3 = 1 };
+
+/* A cache: K and V of n_heads KV heads over n_slots token slots. */
+typedef struct {
+  int32_t format;   /* JET_QCACHE_INT8 or JET_QCACHE_E4M3 */
+  int32_t block;    /* tokens that share a scale: 16, 32, 64 or 128 */
+  int32_t n_heads;  /* KV heads, 1 .. 1024 */
+  int32_t head_dim; /* 64, 128 or 256 */
+  int64_t n_slots;  /* token slots of each head; a multiple of block */
+  void *k, *v;      /* [n_heads][n_slots][head_dim] bytes, 16-byte aligned */
+  uint8_t *k_exp, *v_exp; /* [n_heads][n_slots / block] */
+} jet_qcache;
+
+/* The sequences of a call. Sequence s holds len[s] tokens, token t in slot
+ * slot0[s] + t; slot0[s] is a multiple of the cache's block and sequences
+ * share no block. The call's rows are the last ones of each sequence: rows
+ * row_offsets[s] .. row_offsets[s + 1] - 1 are its last tokens (n of them:
+ * positions len[s] - n .. len[s] - 1). Slots and offsets outside the cache, or
+ * rows outside [0, n_rows), leave the sequence out; a row at a position below
+ * 0 is left out. */
+typedef struct {
+  int32_t n_seq;      /* 0 .. 65535 */
+  int32_t n_rows;     /* rows of the row arrays; 0 .. 2^30 */
+  int32_t max_rows;   /* most rows of one sequence, and  */
+  int32_t reserved;   /* 0 */
+  int64_t max_len;    /* most tokens of one sequence: both size the launch.
+                         Larger values in row_offsets and len are still worked
+                         off, only slower. */
+  const int64_t *slot0;       /* device, [n_seq] */
+  const int32_t *len;         /* device, [n_seq] */
+  const int32_t *row_offsets; /* device, [n_seq + 1], or NULL: row s is the one
+                                 row of sequence s (n_rows >= n_seq) */
+} jet_qcache_batch;
+
+/* Rows of an array: element (row, head, d) at p[row * row_stride +
+ * head * head_stride + d], strides in elements (>= 0). Vectors are used when
+ * p and both strides are multiples of 16 bytes. */
+typedef struct {
+  void *p;
+  int32_t type;     /* JET_T_* */
+  int32_t reserved; /* 0 */
+  int64_t row_stride, head_stride;
+} jet_rows;
+
+/*
+ * jet_qcache_write - quantise the batch's rows of K and V into the cache.
+ *   k, v: rows of cache->n_heads heads (any JET_T_* type; read only).
+ * A block that the rows reach from its first token on is written anew: what it
+ * held before does not matter. Where the first row lands inside a block, the
+ * sequence's earlier tokens in it stay: the scale is the larger of theirs and
+ * the new rows', and when it grows they are rounded again to its step. Bytes
+ * behind a sequence's last token are left as they were.
+ * Errors: JET_E_INVALID, JET_E_DEVICE.
+ */
+int jet_qcache_write(const jet_qcache *cache, const jet_qcache_batch *batch, const jet_rows *k, const jet_rows *v,
+                     void *hip_stream);
+
+/*
+ * jet_qcache_read - read the batch's rows of K and V back: q 2^e, exact in f32
+ * and bf16 while in range, rounded to nearest even in f16.
+ *   k, v: rows of cache->n_heads heads, written. Rows of no sequence are left
+ *   as they were.
+ * Errors: JET_E_INVALID, JET_E_DEVICE.
+ */
+int jet_qcache_read(const jet_qcache *cache, const jet_qcache_batch *batch, const jet_rows *k, const jet_rows *v,
+                    void *hip_stream);
+
+/*
+ * jet_qcache_attention - attention of the batch's rows over the cache (which
+ * holds the rows' own tokens already).
+ *   n_q_heads: a multiple of cache->n_heads; query head h reads KV head
+ *     h / (n_q_heads / cache->n_heads). At most 64 query heads a KV head.
+ *   scale: finite; scores are scale * q . k.
+ *   causal: 1: a row sees the tokens up to its own; 0: it sees all len[s].
+ *   q: rows of n_q_heads heads, JET_T_F16 or JET_T_BF16.
+ *   out: rows of n_q_heads heads, of q's type or JET_T_F32. A row that sees no
+ *     token gets zeros. Rows of no sequence are left as they were.
+ *   lse: device, float[n_rows * n_q_heads] or NULL: ln of the sum of e^score
+ *     of each (row, head); -inf for a row that sees no token.
+ *   workspace: device, 16-byte aligned, at least the bytes that
+ *     jet_qcache_attention_workspace gives for this batch (which may be 0,
+ *     then NULL is fine). Nothing is kept in it between calls.
+ * Scores, maxima, sums and outputs are held in 32 bits; probabilities are
+ * rounded to f16 for the product with V.
+ * Errors: JET_E_INVALID, JET_E_DEVICE.
+ */
+int jet_qcache_attention(const jet_qcache *cache, const jet_qcache_batch *batch, int32_t n_q_heads, float scale,
+                         int32_t causal, const jet_rows *q, const jet_rows *out, float *lse, void *workspace,
+                         int64_t workspace_bytes, void *hip_stream);
+
+/* Bytes of workspace that jet_qcache_attention needs for this batch (its
+ * counts and bounds; the device arrays are not read). Host only. */
+int jet_qcache_attention_workspace(const jet_qcache *cache, const jet_qcache_batch *batch, int32_t n_q_heads,
+                                   int64_t *out_bytes);
+
+/*
+ * jet_logits_adjust - the rules of constrained sampling on a step's logits.
+ * For token v of row r, with seen = v is in the row's history, c = how often v
+ * is in the part of the history behind its first hist_prompt[r] tokens:
+ *   z = logits[r][v];  if seen: z = z > 0 ? z / repetition[r] : z * repetition[r];
+ *   z -= frequency[r] * c + (c > 0 ? presence[r] : 0);
+ *   z += the sum of the row's biases of v, in list order;
+ *   if the row's mask does not allow v: z = -inf (whatever z was, NaN too).
+ * Computed in f32 and rounded once. Ids outside [0, vocab) are ignored. */
+typedef struct {
+  int32_t n_rows, vocab;      /* 0 .. 2^20, 1 .. 2^24 */
+  int32_t type;               /* JET_T_*: of logits and out */
+  int32_t n_masks;            /* rows of masks (0 without) */
+  const void *logits;         /* device, [n_rows][row_stride] */
+  void *out;                  /* device, [n_rows][out_stride]; may be logits
+                                 (with the same stride), else no overlap */
+  int64_t row_stride, out_stride; /* elements, >= vocab */
+  const int32_t *hist_offsets;    /* device, [n_rows + 1], or NULL: no history */
+  const int32_t *hist_ids;        /* device, [n_hist] */
+  const int32_t *hist_prompt;     /* device, [n_rows], or NULL: 0 */
+  int64_t n_hist;                 /* ids in hist_ids (< 2^31) */
+  const float *repetition;        /* device, [n_rows], > 0, or NULL: 1 */
+  const float *presence, *frequency; /* device, [n_rows], or NULL: 0 */
+  const int32_t *bias_offsets;    /* device, [n_rows + 1], or NULL: no biases */
+  const int32_t *bias_ids;        /* device, [n_bias] */
+  const float *bias_values;       /* device, [n_bias] */
+  int64_t n_bias;                 /* < 2^31 */
+  const uint32_t *masks;          /* device, [n_masks][mask_stride], or NULL: bit
+                                     v % 32 of word v / 32 allows token v */
+  int64_t mask_stride;            /* words, >= ceil(vocab / 32) */
+  const int32_t *mask_index;      /* device, [n_rows]: the row's mask, or < 0:
+                                     all allowed; NULL: mask r for row r
+                                     (n_masks >= n_rows). An index >= n_masks
+                                     allows nothing. */
+} jet_logits_args;
+int jet_logits_adjust(const jet_logits_args *args, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,176 @@
+// Attention cache in 8 bits: rows of K and V quantised as they are written, and
+// read back.
+//
+// A block of B tokens of one head has one scale 2^e (byte e + 127). Writing is
+// a maximum over the block's new values and a rounding of each:
+//   e = least (>= -60) with max|x| <= top 2^e, top = 127 (int8) or 448 (e4m3)
+//   q = rne(x 2^-e); where earlier tokens of the sequence share the block,
+//   e = max(e, e_old) and, if it grew, q_old = rne(q_old 2^(e_old - e)).
+// 2^-e is exact, so every value is rounded once; an earlier value that goes
+// through several growths is off by less than 2^e (1/2 + 1/4 + ... steps).
+// Memory bound: rows read once, one byte written for each value.
+#include <algorithm>
+
+#include "qcache.h"
+
+namespace jetk {
+
+// Eight consecutive values of a row from element i.
+template <typename T, bool VEC> __device__ __forceinline__ void load8(float (&x)[8], const T *p) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    const uint4 u = ld16(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] & 0xffff)));
+      x[2 * j + 1] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] >> 16)));
+    }
+  } else if constexpr (VEC) {
+    const uint4 u = ld16(p), w = ld16(p + 4);
+    x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+    x[4] = __uint_as_float(w.x); x[5] = __uint_as_float(w.y); x[6] = __uint_as_float(w.z); x[7] = __uint_as_float(w.w);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = to_f<T>(p[j]);
+  }
+}
+template <typename T, bool VEC> __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    st16(p, make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])));
+  } else if constexpr (VEC) {
+    st16(p, __builtin_bit_cast(uint4, f32x4{x[0], x[1], x[2], x[3]}));
+    st16(p + 4, __builtin_bit_cast(uint4, f32x4{x[4], x[5], x[6], x[7]}));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = from_f<T>(x[j]);
+  }
+}
+template <int FMT> __device__ __forceinline__ void unpack8x8(float (&x)[8], uint2 w) {
+  x[0] = unpack8<FMT, 0>(w.x); x[1] = unpack8<FMT, 1>(w.x); x[2] = unpack8<FMT, 2>(w.x); x[3] = unpack8<FMT, 3>(w.x);
+  x[4] = unpack8<FMT, 0>(w.y); x[5] = unpack8<FMT, 1>(w.y); x[6] = unpack8<FMT, 2>(w.y); x[7] = unpack8<FMT, 3>(w.y);
+}
+
+// One workgroup per (block that a sequence's rows touch, head of K or of V,
+// sequence): it owns the block, so nothing is shared between workgroups.
+template <typename T, int FMT, bool VEC>
+__global__ __launch_bounds__(256) void qcache_write_kernel(QCache c, QBatch b, QRows rk, QRows rv) {
+  __shared__ uint32_t wmax[4];
+  const int tid = threadIdx.x, h = blockIdx.y >> 1;
+  const bool isv = blockIdx.y & 1;
+  const QSeq s = qseq(b, c, blockIdx.z);
+  if (s.lo >= s.hi) return;
+  const int B = 1 << c.lb, hd = c.hd, cpr = hd / 8;  // chunks of 8 values per row
+  const QRows &r = isv ? rv : rk;
+  uint8_t *data = (isv ? c.v : c.k) + ((int64_t)h * c.S + s.slot0) * hd;
+  uint8_t *exps = (isv ? c.ve : c.ke) + (int64_t)h * (c.S >> c.lb) + (s.slot0 >> c.lb);
+  const int b0 = s.lo >> c.lb, b1 = (s.hi - 1) >> c.lb;
+  for (int blk = b0 + blockIdx.x; blk <= b1; blk += gridDim.x) {
+    const int first = blk << c.lb, lo = max(s.lo, first), hi = min(s.hi, first + B);  // the block's new tokens
+    const T *src = (const T *)r.p + (int64_t)(s.row0 + lo - s.pos0) * r.rs + (int64_t)h * r.hs;
+    const int n = (hi - lo) * cpr;
+    uint32_t top = 0;  // float bits of |x| order like the values, NaN and infinity above all
+    for (int i = tid; i < n; i += 256) {
+      float x[8];
+      load8<T, VEC>(x, src + (int64_t)(i / cpr) * r.rs + i % cpr * 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+    }
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    if ((tid & 63) == 0) wmax[tid >> 6] = top;
+    const int old = lo > first ? exps[blk] : 0;  // scale byte of the block's earlier tokens
+    __syncthreads();
+    top = max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3]));
+    const int e = max(scale_byte<FMT>(top), old);
+    const float down = e == kExpNaN ? 0.0f : pow2i(kExpBias - e);
+    for (int i = tid; i < n; i += 256) {
+      float x[8];
+      load8<T, VEC>(x, src + (int64_t)(i / cpr) * r.rs + i % cpr * 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = e == kExpNaN ? 0.0f : x[j] * down;
+      uint2 w = make_uint2(pack8x4<FMT>(x[0], x[1], x[2], x[3]), pack8x4<FMT>(x[4], x[5], x[6], x[7]));
+      *reinterpret_cast<uint2 *>(data + (int64_t)lo * hd + (int64_t)i * 8) = w;
+    }
+    if (e > old && lo > first && e != kExpNaN) {  // the earlier tokens' scale grew
+      for (int i = tid; i < (lo - first) * cpr; i += 256) {
+        uint2 *p = reinterpret_cast<uint2 *>(data + (int64_t)first * hd + (int64_t)i * 8);
+        float x[8];
+        unpack8x8<FMT>(x, *p);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = ldexpf(x[j], old - e);
+        *p = make_uint2(pack8x4<FMT>(x[0], x[1], x[2], x[3]), pack8x4<FMT>(x[4], x[5], x[6], x[7]));
+      }
+    }
+    __syncthreads();  // wmax and the old scale have been read
+    if (tid == 0) exps[blk] = (uint8_t)e;
+  }
+}
+
+// One workgroup per (run of tokens, head of K or of V, sequence).
+constexpr int kReadTokens = 32;
+template <typename T, int FMT, bool VEC>
+__global__ __launch_bounds__(256) void qcache_read_kernel(QCache c, QBatch b, QRows rk, QRows rv) {
+  const int tid = threadIdx.x, h = blockIdx.y >> 1;
+  const bool isv = blockIdx.y & 1;
+  const QSeq s = qseq(b, c, blockIdx.z);
+  const int hd = c.hd, cpr = hd / 8;
+  const QRows &r = isv ? rv : rk;
+  const uint8_t *data = (isv ? c.v : c.k) + ((int64_t)h * c.S + s.slot0) * hd;
+  const uint8_t *exps = (isv ? c.ve : c.ke) + (int64_t)h * (c.S >> c.lb) + (s.slot0 >> c.lb);
+  for (int64_t t0 = s.lo + (int64_t)blockIdx.x * kReadTokens; t0 < s.hi; t0 += (int64_t)gridDim.x * kReadTokens) {
+    const int n = min(kReadTokens, s.hi - (int)t0) * cpr;
+    for (int i = tid; i < n; i += 256) {
+      const int t = (int)t0 + i / cpr, d = i % cpr * 8;
+      const int e = exps[t >> c.lb];
+      float x[8];
+      unpack8x8<FMT>(x, *reinterpret_cast<const uint2 *>(data + (int64_t)t * hd + d));
+      const float up = e == kExpNaN ? __uint_as_float(0x7fc00000u) : pow2i(e - kExpBias);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= up;
+      store8<T, VEC>((T *)r.p + (int64_t)(s.row0 + t - s.pos0) * r.rs + (int64_t)h * r.hs + d, x);
+    }
+  }
+}
+
+// Launch over (x, head of K or V, sequence); kernels walk on where a sequence
+// has more rows than the grid was sized for.
+#define JETK_QROWS(KERNEL)                                                                                        \
+  do {                                                                                                            \
+    const bool vec = k.vec && v.vec;                                                                              \
+    if (c.fmt == 0 && vec) hipLaunchKernelGGL((KERNEL<T, 0, true>), grid, dim3(256), 0, st, c, b, k, v);          \
+    else if (c.fmt == 0) hipLaunchKernelGGL((KERNEL<T, 0, false>), grid, dim3(256), 0, st, c, b, k, v);           \
+    else if (vec) hipLaunchKernelGGL((KERNEL<T, 1, true>), grid, dim3(256), 0, st, c, b, k, v);                   \
+    else hipLaunchKernelGGL((KERNEL<T, 1, false>), grid, dim3(256), 0, st, c, b, k, v);                           \
+  } while (0)
+
+template <typename T>
+static hipError_t write_t(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
+  const int64_t blocks = ((int64_t)std::max(b.max_rows, 1) + (1 << c.lb) - 2) / (1 << c.lb) + 1;
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, 65536), (unsigned)(2 * c.H), (unsigned)b.n_seq);
+  JETK_QROWS(qcache_write_kernel);
+  return hipGetLastError();
+}
+template <typename T>
+static hipError_t read_t(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
+  const int64_t runs = ((int64_t)std::max(b.max_rows, 1) + kReadTokens - 1) / kReadTokens;
+  const dim3 grid((unsigned)std::min<int64_t>(runs, 65536), (unsigned)(2 * c.H), (unsigned)b.n_seq);
+  JETK_QROWS(qcache_read_kernel);
+  return hipGetLastError();
+}
+
+hipError_t launch_qcache_write(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
+  if (b.n_seq <= 0 || b.n_rows <= 0 || c.S <= 0) return hipSuccess;
+  if (k.type != v.type) return hipErrorInvalidValue;
+  if (k.type == 0) return write_t<float>(c, b, k, v, st);
+  if (k.type == 1) return write_t<f16>(c, b, k, v, st);
+  return write_t<bf16>(c, b, k, v, st);
+}
+
+hipError_t launch_qcache_read(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
+  if (b.n_seq <= 0 || b.n_rows <= 0 || c.S <= 0) return hipSuccess;
+  if (k.type != v.type) return hipErrorInvalidValue;
+  if (k.type == 0) return read_t<float>(c, b, k, v, st);
+  if (k.type == 1) return read_t<f16>(c, b, k, v, st);
+  return read_t<bf16>(c, b, k, v, st);
+}
+
+}  // namespace jetk

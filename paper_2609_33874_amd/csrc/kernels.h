@@ -261,4 +261,56 @@ hipError_t launch_gemm_grouped(int dtype, int bm, int epi, const void *A, int64_
                                int64_t group_stride, const int *tile_group, int M, int N, int K, void *out,
                                int64_t ldo, float oscale, hipStream_t st);
 
+// ---- attention cache in 8 bits (k_qcache.hip, k_qattn.hip) ----
+// The structs of jet.h as kernels take them: type 0 = f32, 1 = f16, 2 = bf16;
+// vec: rows can be moved in 16-byte vectors.
+struct QCache {
+  int fmt, lb, H, hd;  // format, log2 of the block's tokens, KV heads, head_dim
+  int64_t S;           // slots per head
+  uint8_t *k, *v, *ke, *ve;
+};
+struct QBatch {
+  int n_seq, n_rows, max_rows;
+  int64_t max_len;
+  const int64_t *slot0;
+  const int32_t *len, *rows;
+};
+struct QRows {
+  void *p;
+  int type, vec;
+  int64_t rs, hs;
+};
+// The batch's rows of k and v into the cache, and back out of it.
+hipError_t launch_qcache_write(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st);
+hipError_t launch_qcache_read(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st);
+struct QAttn {
+  QCache c;
+  QBatch b;
+  QRows q, out;
+  int Hq, causal;
+  float scale;
+  float *lse;   // [n_rows][Hq] or NULL
+  void *ws;     // qattn_workspace bytes
+};
+int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq);
+hipError_t launch_qattn(const QAttn &a, hipStream_t st);
+
+// ---- logits of a decode step (k_logits.hip) ----
+struct LogitsArgs {
+  int R, V, type, n_masks;
+  const void *in;
+  void *out;
+  int64_t in_ld, out_ld;
+  const int32_t *h_off, *h_ids, *h_prompt;
+  int n_hist;
+  const float *rep, *pres, *freq;
+  const int32_t *b_off, *b_ids;
+  const float *b_val;
+  int n_bias;
+  const uint32_t *masks;
+  int64_t mask_ld;
+  const int32_t *mask_index;
+};
+hipError_t launch_logits_adjust(const LogitsArgs &a, hipStream_t st);
+
 }  // namespace jetk

@@ -21,6 +21,8 @@ JET_CHOICE, JET_BINARY, JET_ORDINAL = 0, 1, 2
 JET_FLAG_KERNEL_TIMING = 1
 JET_FLAG_RECORD_ROUTES = 2
 JET_NOALLOC_SCRATCH_BYTES = 64 << 20
+JET_T_F32, JET_T_F16, JET_T_BF16 = 0, 1, 2
+JET_QCACHE_INT8, JET_QCACHE_E4M3 = 0, 1
 KERNEL_CLASSES = ["gemm_qkv", "gemm_o", "gemm_gateup", "gemm_down", "lmhead", "attn_prefix",
                   "attn_cand", "gdn", "other"]
 ERROR_NAMES = {1: "JET_E_INVALID", 2: "JET_E_CAPACITY", 3: "JET_E_OOM", 4: "JET_E_DEVICE", 5: "JET_E_IO"}
@@ -29,7 +31,9 @@ ERROR_NAMES = {1: "JET_E_INVALID", 2: "JET_E_CAPACITY", 3: "JET_E_OOM", 4: "JET_
 EXPORTS = ["jet_model_load", "jet_prefill_prefix", "jet_generate_trace", "jet_score_candidates",
            "jet_score_candidates_noalloc", "jet_decide",
            "jet_answer_classes", "jet_evaluate", "jet_candidate_layout", "jet_stats_get", "jet_stats_reset", "jet_model_info",
-           "jet_routes_get", "jet_prefix_free", "jet_model_free", "jet_last_error"]
+           "jet_routes_get", "jet_prefix_free", "jet_model_free", "jet_last_error",
+           "jet_qcache_write", "jet_qcache_read", "jet_qcache_attention", "jet_qcache_attention_workspace",
+           "jet_logits_adjust"]
 
 
 class JetError(RuntimeError):
@@ -52,6 +56,34 @@ class jet_stats(ctypes.Structure):
                 ("score_waves", ctypes.c_int64), ("kernel_launches", ctypes.c_int64 * 9),
                 ("kernel_ms", ctypes.c_double * 9), ("kernel_flops", ctypes.c_double * 9),
                 ("kernel_bytes", ctypes.c_double * 9)]
+
+
+class jet_qcache(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("block", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_slots", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p)]
+
+
+class jet_qcache_batch(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("max_len", ctypes.c_int64), ("slot0", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("row_offsets", ctypes.c_void_p)]
+
+
+class jet_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class jet_logits_args(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("n_masks", ctypes.c_int32), ("logits", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("row_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("hist_offsets", ctypes.c_void_p),
+                ("hist_ids", ctypes.c_void_p), ("hist_prompt", ctypes.c_void_p), ("n_hist", ctypes.c_int64),
+                ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("bias_offsets", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int64), ("masks", ctypes.c_void_p), ("mask_stride", ctypes.c_int64),
+                ("mask_index", ctypes.c_void_p)]
 
 
 _lib = None
@@ -85,6 +117,12 @@ def lib() -> ctypes.CDLL:
         L.jet_stats_reset.argtypes = [P]
         L.jet_model_info.argtypes = [P, P, P, P, P, P]
         L.jet_routes_get.argtypes = [P, I32, P, P, P, P, I64]
+        qc, qb, rows = ctypes.POINTER(jet_qcache), ctypes.POINTER(jet_qcache_batch), ctypes.POINTER(jet_rows)
+        L.jet_qcache_write.argtypes = [qc, qb, rows, rows, P]
+        L.jet_qcache_read.argtypes = [qc, qb, rows, rows, P]
+        L.jet_qcache_attention.argtypes = [qc, qb, I32, ctypes.c_float, I32, rows, rows, P, P, I64, P]
+        L.jet_qcache_attention_workspace.argtypes = [qc, qb, I32, ctypes.POINTER(I64)]
+        L.jet_logits_adjust.argtypes = [ctypes.POINTER(jet_logits_args), P]
         L.jet_prefix_free.argtypes = [P]
         L.jet_prefix_free.restype = None
         L.jet_model_free.argtypes = [P]
@@ -281,3 +319,197 @@ def jet_prefix_free(prefix) -> None:
 
 def jet_model_free(model) -> None:
     lib().jet_model_free(model)
+
+
+# ---------------------------------------------------------------------------
+# Operators on device arrays: torch tensors on one GPU. Work is enqueued on
+# `stream` (a raw hipStream_t), by default torch's current stream of that GPU.
+# ---------------------------------------------------------------------------
+
+def _device_array(t, name, dtype, device, shape=None, contiguous=True):
+    """Pointer of a torch tensor on `device` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name} must be {dtype} on {device}")
+    if contiguous and not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t.data_ptr() or None
+
+
+def _type_of(t, name):
+    import torch
+    ty = {torch.float32: JET_T_F32, torch.float16: JET_T_F16, torch.bfloat16: JET_T_BF16}.get(t.dtype)
+    if ty is None:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16")
+    return ty
+
+
+def _rows(t, name, heads, head_dim, device):
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
+        raise ValueError(f"{name} must have shape [rows, {heads}, {head_dim}], not {list(t.shape)}")
+    if t.device != device:
+        raise TypeError(f"{name} must be on {device}")
+    if t.stride(2) != 1:
+        raise TypeError(f"{name} must have its last dimension contiguous")
+    return jet_rows(t.data_ptr() or None, _type_of(t, name), 0, t.stride(0), t.stride(1))
+
+
+def _stream(stream, device):
+    if stream is not None:
+        return stream
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+class QCache:
+    """An 8-bit attention cache over four tensors that the caller keeps: k and
+    v, one byte a value, [heads, slots, head_dim]; k_exp and v_exp, uint8,
+    [heads, slots // block]. `QCache.empty` makes them."""
+
+    def __init__(self, k, v, k_exp, v_exp, block: int = 32, format: int = JET_QCACHE_INT8):
+        import torch
+        if k.dim() != 3 or k.element_size() != 1:
+            raise TypeError("k must hold bytes, [heads, slots, head_dim]")
+        H, S, hd = k.shape
+        if not k.is_cuda:
+            raise TypeError("the cache must be on a GPU")
+        if v.element_size() != 1 or v.device != k.device or v.shape != k.shape:
+            raise TypeError("v must be like k")
+        if not (k.is_contiguous() and v.is_contiguous()):
+            raise TypeError("k and v must be contiguous")
+        shape = (H, S // block if block > 0 else 0)
+        self.device = k.device
+        self.tensors = (k, v, k_exp, v_exp)
+        self.c = jet_qcache(format, block, H, hd, S, k.data_ptr() or None, v.data_ptr() or None,
+                            _device_array(k_exp, "k_exp", torch.uint8, k.device, shape),
+                            _device_array(v_exp, "v_exp", torch.uint8, k.device, shape))
+
+    @classmethod
+    def empty(cls, heads: int, slots: int, head_dim: int, block: int = 32, format: int = JET_QCACHE_INT8,
+              device="cuda"):
+        import torch
+        k, v = (torch.empty((heads, slots, head_dim), dtype=torch.int8, device=device) for _ in "kv")
+        ke, ve = (torch.empty((heads, slots // block), dtype=torch.uint8, device=device) for _ in "kv")
+        return cls(k, v, ke, ve, block, format)
+
+
+def _batch(cache, slot0, length, n_rows, row_offsets, max_rows, max_len):
+    import torch
+    n = slot0.shape[0]
+    if row_offsets is None:
+        off, most = None, 1
+    else:
+        off, most = _device_array(row_offsets, "row_offsets", torch.int32, cache.device, (n + 1,)), n_rows
+    return jet_qcache_batch(n, n_rows, most if max_rows is None else max_rows, 0,
+                            cache.c.n_slots if max_len is None else max_len,
+                            _device_array(slot0, "slot0", torch.int64, cache.device, (n,)),
+                            _device_array(length, "length", torch.int32, cache.device, (n,)), off)
+
+
+def _move_rows(fn, cache, slot0, length, k, v, row_offsets, max_rows, stream):
+    H, hd = cache.c.n_heads, cache.c.head_dim
+    rk, rv = _rows(k, "k", H, hd, cache.device), _rows(v, "v", H, hd, cache.device)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("k and v have different numbers of rows")
+    b = _batch(cache, slot0, length, k.shape[0], row_offsets, max_rows, None)
+    _check(fn(ctypes.byref(cache.c), ctypes.byref(b), ctypes.byref(rk), ctypes.byref(rv),
+              _stream(stream, cache.device)))
+
+
+def jet_qcache_write(cache: QCache, slot0, length, k, v, row_offsets=None, max_rows=None, stream=None) -> None:
+    """Quantises rows of k and v ([rows, heads, head_dim]) into the cache: the
+    last tokens of each sequence (slot0 int64, length int32, both [n_seq];
+    row_offsets int32 [n_seq + 1], None: one row each)."""
+    _move_rows(lib().jet_qcache_write, cache, slot0, length, k, v, row_offsets, max_rows, stream)
+
+
+def jet_qcache_read(cache: QCache, slot0, length, k, v, row_offsets=None, max_rows=None, stream=None) -> None:
+    """Reads the last tokens of each sequence back into the rows of k and v."""
+    _move_rows(lib().jet_qcache_read, cache, slot0, length, k, v, row_offsets, max_rows, stream)
+
+
+def jet_qcache_attention_workspace(cache: QCache, n_seq: int, n_q_heads: int, n_rows=None, max_rows: int = 1,
+                                   max_len=None) -> int:
+    """Bytes of workspace that jet_qcache_attention needs for such a batch."""
+    b = jet_qcache_batch(n_seq, n_seq * max_rows if n_rows is None else n_rows, max_rows, 0,
+                         cache.c.n_slots if max_len is None else max_len, None, None, None)
+    n = ctypes.c_int64()
+    _check(lib().jet_qcache_attention_workspace(ctypes.byref(cache.c), ctypes.byref(b), n_q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def jet_qcache_attention(cache: QCache, slot0, length, q, out, row_offsets=None, max_rows=None, max_len=None,
+                         causal: bool = True, scale=None, lse=None, workspace=None, stream=None):
+    """Attention of q ([rows, n_q_heads, head_dim], float16 or bfloat16) over the
+    cache into `out` (q's type or float32), the rows being the last tokens of
+    each sequence; lse: float32 [rows, n_q_heads] or None. scale: 1 /
+    sqrt(head_dim) by default. workspace: a uint8 tensor of at least
+    jet_qcache_attention_workspace bytes (None: one is allocated). Returns out."""
+    import torch
+    dev, hd = cache.device, cache.c.head_dim
+    if q.dim() != 3 or out.shape != q.shape:
+        raise ValueError("q and out must have shape [rows, n_q_heads, head_dim]")
+    R, Hq = q.shape[0], q.shape[1]
+    rq, ro = _rows(q, "q", Hq, hd, dev), _rows(out, "out", Hq, hd, dev)
+    b = _batch(cache, slot0, length, R, row_offsets, max_rows, max_len)
+    st = _stream(stream, dev)
+    if workspace is None:
+        n = ctypes.c_int64()
+        _check(lib().jet_qcache_attention_workspace(ctypes.byref(cache.c), ctypes.byref(b), Hq, ctypes.byref(n)))
+        if n.value:
+            workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+            if stream is not None:  # keep its memory until that stream's work is done
+                workspace.record_stream(torch.cuda.ExternalStream(stream, device=dev))
+    ws, ws_n = (None, 0) if workspace is None else (_device_array(workspace, "workspace", torch.uint8, dev),
+                                                    workspace.numel())
+    _check(lib().jet_qcache_attention(ctypes.byref(cache.c), ctypes.byref(b), Hq,
+                                      hd ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(rq),
+                                      ctypes.byref(ro),
+                                      _device_array(lse, "lse", torch.float32, dev, (R, Hq)), ws, ws_n, st))
+    return out
+
+
+def jet_logits_adjust(logits, out=None, history=None, hist_prompt=None, repetition=None, presence=None,
+                      frequency=None, bias=None, masks=None, mask_index=None, stream=None):
+    """Penalties for repeated tokens, biases and masks on logits [rows, vocab]
+    (float32, float16 or bfloat16, any row stride). out: where to write (None:
+    in place). history: (offsets int32 [rows + 1], ids int32); hist_prompt:
+    int32 [rows], how many of a row's ids are its prompt. repetition, presence,
+    frequency: float32 [rows]. bias: (offsets int32 [rows + 1], ids int32,
+    values float32). masks: int32 [n_masks, words], bit v % 32 of word v / 32
+    allows token v; mask_index: int32 [rows], < 0 for none. Returns out."""
+    import torch
+    out = logits if out is None else out
+    if logits.dim() != 2 or out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("logits and out must be [rows, vocab] of one type")
+    dev, (R, V) = logits.device, logits.shape
+    if not logits.is_cuda or out.device != dev:
+        raise TypeError("logits and out must be on one GPU")
+    if V > 1 and (logits.stride(1) != 1 or out.stride(1) != 1):
+        raise TypeError("logits and out must have contiguous rows")
+    ld = lambda t: max(t.stride(0), V) if R <= 1 else t.stride(0)  # noqa: E731
+    i32, f32 = torch.int32, torch.float32
+    a = jet_logits_args(n_rows=R, vocab=V, type=_type_of(logits, "logits"), logits=logits.data_ptr() or None,
+                        out=out.data_ptr() or None, row_stride=ld(logits), out_stride=ld(out))
+    if history is not None:
+        a.hist_offsets = _device_array(history[0], "history offsets", i32, dev, (R + 1,))
+        a.hist_ids, a.n_hist = _device_array(history[1], "history ids", i32, dev), history[1].numel()
+    a.hist_prompt = _device_array(hist_prompt, "hist_prompt", i32, dev, (R,))
+    a.repetition = _device_array(repetition, "repetition", f32, dev, (R,))
+    a.presence = _device_array(presence, "presence", f32, dev, (R,))
+    a.frequency = _device_array(frequency, "frequency", f32, dev, (R,))
+    if bias is not None:
+        a.bias_offsets = _device_array(bias[0], "bias offsets", i32, dev, (R + 1,))
+        a.bias_ids, a.n_bias = _device_array(bias[1], "bias ids", i32, dev), bias[1].numel()
+        a.bias_values = _device_array(bias[2], "bias values", f32, dev, (a.n_bias,))
+    if masks is not None:
+        if masks.dim() != 2:
+            raise ValueError("masks must be [n_masks, words]")
+        a.masks, a.n_masks = _device_array(masks, "masks", i32, dev), masks.shape[0]
+        a.mask_stride = masks.shape[1]
+    a.mask_index = _device_array(mask_index, "mask_index", i32, dev, (R,))
+    _check(lib().jet_logits_adjust(ctypes.byref(a), _stream(stream, dev)))
+    return out

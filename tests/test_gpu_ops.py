@@ -1,0 +1,681 @@
+"""GPU: the operators on device arrays (8-bit attention cache, logit rules)
+against 64-bit references on the CPU.
+
+Quantised values, scales and whole numbers have to be equal. Tolerances of
+attention, for one output, with u = 2^-24 and the scores in 32 bits:
+  * a score is a sum of hd products (q and the 8-bit values are exact in f16, a
+    product in f32), the scales are powers of two, and one product with scale *
+    log2 e (rounded twice): |ds| <= (hd + 6) u |scale| sum_d |q_d k_jd|. The
+    probability then moves by the factor e^ds, and the weights p / l by e^2ds.
+  * exp2 of a f32 difference, the sums over n keys and their rescaling: (n + 64) u
+    relative (64: a rescaling for each of many splits, the exponential's own ulps)
+  * a probability is rounded to f16 (relative 2^-11), or below 2^-24 of f16's
+    range (its largest is kept at 2^15): 2^-40 of the largest scale met, a key;
+    the sum l is of the unrounded ones
+  * the output is rounded once: half a step of its type.
+"""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import _qcache_ref as ref
+from paper_2609_33874_amd import jet as J
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+TORCH = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def log(msg):
+    print(msg, file=sys.__stderr__, flush=True)
+
+
+def i32(x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def i64(x):
+    return torch.tensor(list(x), dtype=torch.int64, device=DEV)
+
+
+def offsets(n):
+    return [0] + list(np.cumsum(n))
+
+
+def layout(lens, block, gap=0):
+    """First slots of sequences of these lengths (every other one `gap` blocks on), and the slots in all."""
+    at, out = 0, []
+    for i, n in enumerate(lens):
+        at += block * gap * (i % 2)
+        out.append(at)
+        at += (n + block - 1) // block * block
+    return out, max(at, block)
+
+
+def values(rng, shape, spread=1.0):
+    """Rows with large and small tokens and channels."""
+    x = rng.normal(size=shape) * np.exp(0.7 * rng.normal(size=shape[-1]))
+    return x * np.exp(spread * rng.normal(size=shape[:-1]))[..., None]
+
+
+class Pair:
+    """A cache on the GPU and its reference on the CPU, written alike."""
+
+    def __init__(self, lens, H, hd, block, fmt, gap=0, extra=0):
+        self.lens, self.H, self.hd, self.block, self.fmt = lens, H, hd, block, fmt
+        self.slot0, slots = layout(lens, block, gap)
+        self.slots = slots + extra * block
+        g = torch.Generator(device=DEV)
+        g.manual_seed(5)
+        rnd = lambda shape: torch.randint(0, 256, shape, generator=g, dtype=torch.uint8, device=DEV)  # noqa: E731
+        # what nobody wrote holds any bytes
+        self.kb, self.vb = rnd((H, self.slots, hd)), rnd((H, self.slots, hd))
+        self.ke, self.ve = rnd((H, self.slots // block)), rnd((H, self.slots // block))
+        self.gpu = J.QCache(self.kb, self.vb, self.ke, self.ve, block, fmt)
+        self.k, self.v = ([ref.RefCache(self.slots, hd, block, fmt) for _ in range(H)] for _ in "kv")
+
+    def write(self, held, k, v, rows=None, seqs=None, **kw):
+        """k, v: torch rows [R, H, hd] on the GPU; held[s] tokens are there already, rows[s] join them."""
+        seqs = range(len(self.lens)) if seqs is None else seqs
+        rows = [1] * len(seqs) if rows is None else rows
+        J.jet_qcache_write(self.gpu, i64(self.slot0[s] for s in seqs), i32(h + n for h, n in zip(held, rows)), k, v,
+                           row_offsets=i32(offsets(rows)), **kw)
+        kn, vn = k.double().cpu().numpy(), v.double().cpu().numpy()
+        r = 0
+        for s, h, n in zip(seqs, held, rows):
+            for i in range(self.H):
+                self.k[i].write(self.slot0[s], h, kn[r:r + n, i])
+                self.v[i].write(self.slot0[s], h, vn[r:r + n, i])
+            r += n
+
+    def fill(self, rng, src="f16", spread=1.0):
+        n = sum(self.lens)
+        k, v = (torch.tensor(values(rng, (n, self.H, self.hd), spread)).to(TORCH[src]).to(DEV) for _ in "kv")
+        self.write([0] * len(self.lens), k, v, self.lens)
+
+    def check(self, lens=None):
+        """Every token of every sequence, read back in 32 bits, and every scale."""
+        lens = self.lens if lens is None else lens
+        R = sum(lens)
+        k, v = (torch.full((R + 2, self.H, self.hd), 7.0, device=DEV) for _ in "kv")
+        J.jet_qcache_read(self.gpu, i64(self.slot0), i32(lens), k, v, row_offsets=i32(offsets(lens)))
+        for got, want, e in ((k, self.k, self.ke), (v, self.v, self.ve)):
+            got, e = got.double().cpu().numpy(), e.cpu().numpy()
+            assert np.all(got[R:] == 7.0)  # rows behind the last sequence
+            r = 0
+            for s, n in zip(self.slot0, lens):
+                for h in range(self.H):
+                    # (in f32, where 64 2^122, the 8-bit value nearest to f32's largest, is infinite)
+                    with np.errstate(over="ignore"):
+                        x = want[h].values(s, n).astype(np.float32)
+                    np.testing.assert_array_equal(got[r:r + n, h], x)
+                    for b in range(s // self.block, (s + n + self.block - 1) // self.block):
+                        x = want[h].e[b]
+                        assert e[h, b] == (255 if x is None else x + 127)
+                r += n
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("src,hd,block", [("f16", 128, 32), ("bf16", 128, 16), ("f32", 64, 64), ("f16", 256, 128),
+                                          ("f32", 256, 128), ("bf16", 64, 16)])
+def test_write_and_read_prompts(fmt, src, hd, block):
+    rng = np.random.default_rng(1)
+    lens = [1, block - 1, block, block + 1, 0, 3 * block + 5, 200]
+    p = Pair(lens, 2, hd, block, fmt, gap=1, extra=2)
+    p.fill(rng, src)
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("block", [16, 32, 128])
+def test_append_tokens_whose_scale_grows(fmt, block):
+    """Tokens one and a few at a time; each larger than the last for a while, so that scales grow inside a block."""
+    rng = np.random.default_rng(2)
+    p = Pair([300, 77, 150], 2, 64, block, fmt)
+    held = [0, 0, 0]
+    step = 0
+    while any(h < n for h, n in zip(held, p.lens)):
+        seqs = [s for s in range(3) if held[s] < p.lens[s]]
+        n = [min([1, 3, 1, block, 2][(step + s) % 5], p.lens[s] - held[s]) for s in seqs]
+        x = [torch.tensor(values(rng, (sum(n), 2, 64), 0.3) * 1.3 ** (step % 40)).to(torch.float16).to(DEV)
+             for _ in "kv"]
+        p.write([held[s] for s in seqs], x[0], x[1], n, seqs)
+        for s, m in zip(seqs, n):
+            held[s] += m
+        step += 1
+        if step in (1, 2, 7, 20, 50):
+            p.check(held)
+    p.check()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_values_at_the_edges_of_the_formats(fmt):
+    """Exact ends of a scale, ties, zeros, subnormals, the largest values, growth by many steps."""
+    top = ref.TOP[fmt]
+    nxt = np.nextafter(np.float32(top), np.float32(np.inf))
+    rows = [[top, -top, 0.5, 1.5, 2.5, -0.5, 0.0, -0.0], [nxt, 1.0] * 4, [top / 2, top / 4] * 4, [0.0] * 8,
+            [1e-45, -1e-45, 2e-38, 0, 0, 0, 0, 0], [2.0 ** -70, 2.0 ** -61, 2.0 ** -60, 2.0 ** -54] * 2,
+            [3.4028234e38, -3.4028234e38, 1e38, 1.0, 0, 0, 0, 0], [17.0, 18.0, 19.0, 20.0, 0.0625, 0.03125, 0.001, 447.9]]
+    x = np.zeros((len(rows), 1, 64), np.float32)
+    for i, r in enumerate(rows):
+        x[i, 0] = np.tile(np.array(r, np.float32), 8)
+    for order in (range(len(rows)), reversed(range(len(rows))), (5, 4, 0, 2, 7, 1, 6, 3)):
+        p = Pair([len(rows)], 1, 64, 16, fmt)
+        for n, i in enumerate(order):
+            t = torch.tensor(x[i:i + 1]).to(DEV)
+            p.write([n], t, 2 * t if i != 6 else t)
+            p.check([n + 1])
+    p = Pair([len(rows)], 1, 64, 16, fmt)
+    p.write([0], torch.tensor(x).to(DEV), torch.tensor(x[::-1].copy()).to(DEV), [len(rows)])
+    p.check()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_values_that_are_not_finite_poison_their_block(bad):
+    rng = np.random.default_rng(3)
+    p = Pair([50], 2, 64, 16, 0)
+    k, v = (torch.tensor(values(rng, (50, 2, 64))).to(torch.float32).to(DEV) for _ in "kv")
+    k[20, 1, 63] = bad
+    v[49, 0, 0] = bad
+    p.write([0], k, v, [50])
+    p.check()
+    assert p.k[1].e[1] is None and p.v[0].e[3] is None and p.k[0].e[1] is not None
+    t = torch.ones((1, 2, 64), device=DEV)
+    p.lens[0] = 51
+    p.write([50], t, t)  # a token that joins a poisoned block is lost too, until the block is written anew
+    p.check()
+    p.write([16], k[:16], v[:16], [16])
+    p.check()
+
+
+def test_strides_orders_and_unaligned_rows():
+    rng = np.random.default_rng(4)
+    H, hd, lens = 3, 64, [5, 40, 17]
+    R = sum(lens)
+    for src in ("f16", "f32"):
+        big = torch.tensor(values(rng, (R + 3, 2 * H, hd + 7))).to(TORCH[src]).to(DEV)
+        head_major = big[:R, :H, :hd].transpose(0, 1).contiguous().transpose(0, 1)
+        for k, v in ((big[1:R + 1, :H, :hd], big[2:R + 2, ::2, 3:hd + 3]), (head_major, big[:R, H:, 7:]),
+                     (big[:1, :H, :hd].expand(R, H, hd), big[:R, :1, 1:hd + 1].expand(R, H, hd))):
+            p = Pair(lens, H, hd, 16, 0)
+            p.write([0, 0, 0], k, v, lens)
+            p.check()
+        # read into slices of larger arrays: what lies between stays
+        out = torch.full((R + 2, H + 1, hd + 5), 3.0, dtype=TORCH[src], device=DEV)
+        J.jet_qcache_read(p.gpu, i64(p.slot0), i32(lens), out[1:R + 1, :H, 2:hd + 2], out[1:R + 1, :H, 2:hd + 2],
+                          row_offsets=i32(offsets(lens)))
+        want = torch.full_like(out, 3.0)
+        r = 1
+        for s, n in zip(p.slot0, lens):
+            for h in range(H):
+                # (both of k and v go there: v last or first, so only the untouched places are compared)
+                want[r:r + n, h, 2:hd + 2] = out[r:r + n, h, 2:hd + 2]
+            r += n
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16"])
+def test_read_rounds_once(out):
+    """Part of a sequence's tail, in 16 bits: f16 rounds, overflows and has subnormals; bf16 holds every value."""
+    p = Pair([70], 1, 64, 32, 0)
+    x = np.random.default_rng(6).normal(size=(70, 1, 64)) * np.exp2(np.linspace(-40, 20, 70))[:, None, None]
+    t = torch.tensor(x, dtype=torch.float32).to(DEV)
+    p.write([0], t, -t, [70])
+    k, v = (torch.empty((33, 1, 64), dtype=TORCH[out], device=DEV) for _ in "kv")
+    J.jet_qcache_read(p.gpu, i64(p.slot0), i32([70]), k, v, row_offsets=i32([0, 33]))
+    for got, r in ((k, p.k), (v, p.v)):
+        want = torch.tensor(r[0].values(37, 33)).to(TORCH[out])
+        assert torch.equal(got.cpu()[:, 0], want)
+
+
+def test_sequences_outside_the_cache_are_left_out():
+    """Slots, lengths and offsets that do not fit: nothing is read or written for those sequences."""
+    rng = np.random.default_rng(7)
+    p = Pair([40, 40, 40, 40, 40], 1, 64, 16, 0)
+    p.fill(rng)
+    before = [t.clone() for t in p.gpu.tensors]
+    S = p.slots
+    slot0, lens = i64([-16, 8, S, S - 16, 0]), i32([40, 40, 1, 17, -5])
+    t = torch.ones((10, 1, 64), device=DEV, dtype=torch.float16)
+    J.jet_qcache_write(p.gpu, slot0, lens, t, t, row_offsets=i32([0, 2, 4, 6, 8, 10]))
+    J.jet_qcache_write(p.gpu, i64([0, 48]), i32([40, 40]), t, t, row_offsets=i32([2, 1, 11]))  # decreasing, past the rows
+    J.jet_qcache_write(p.gpu, i64([0]), i32([40]), t, t, row_offsets=i32([-1, 1]))
+    for a, b in zip(before, p.gpu.tensors):
+        assert torch.equal(a, b)
+    out = torch.full((10, 1, 64), 5.0, device=DEV)
+    J.jet_qcache_read(p.gpu, slot0, lens, out, out.clone(), row_offsets=i32([0, 2, 4, 6, 8, 10]))
+    assert torch.all(out == 5.0)
+    q = torch.ones((10, 2, 64), device=DEV, dtype=torch.float16)
+    o, lse = torch.full_like(q, 5.0), torch.full((10, 2), 5.0, device=DEV)
+    J.jet_qcache_attention(p.gpu, slot0, lens, q, o, row_offsets=i32([0, 2, 4, 6, 8, 10]), lse=lse)
+    o, lse = o.cpu(), lse.cpu()
+    assert torch.all((o == 0.0) | (o == 5.0)) and torch.all((lse == 5.0) | (lse == -np.inf))
+    # rows at positions before the first token are left out of a write
+    p.write([0], t[:2], t[:2], [2], [0])
+    J.jet_qcache_write(p.gpu, i64([0]), i32([2]), torch.cat([9 * t[:3], t[:2]]), torch.cat([9 * t[:3], t[:2]]),
+                       row_offsets=i32([0, 5]))
+    p.check([2, 40, 40, 40, 40])
+
+
+def test_more_rows_than_announced_are_worked_off():
+    rng = np.random.default_rng(8)
+    p = Pair([200, 3], 1, 64, 16, 0)
+    k, v = (torch.tensor(values(rng, (203, 1, 64))).to(torch.float16).to(DEV) for _ in "kv")
+    p.write([0, 0], k, v, [200, 3], max_rows=1)
+    p.check()
+    a, b = torch.zeros((203, 1, 64), device=DEV), torch.zeros((203, 1, 64), device=DEV)
+    J.jet_qcache_read(p.gpu, i64(p.slot0), i32(p.lens), a, b, row_offsets=i32([0, 200, 203]), max_rows=2)
+    np.testing.assert_array_equal(a[:200, 0].double().cpu().numpy(), p.k[0].values(0, 200))
+    q = torch.tensor(values(rng, (203, 2, 64), 0.2)).to(torch.float16).to(DEV)
+    check_attention(p, q, [200, 3], True, max_rows=1, max_len=5)
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def check_attention(p, q, rows, causal, out="same", scale=None, lens=None, lse=True, **kw):
+    """One call against the reference, with rows behind the last sequence."""
+    lens = p.lens if lens is None else lens
+    R, Hq, hd = q.shape
+    G = Hq // p.H
+    scale = hd ** -0.5 if scale is None else scale
+    otype = q.dtype if out == "same" else torch.float32
+    o = torch.full((R + 1, Hq, hd), 9.0, dtype=otype, device=DEV)
+    ls = torch.full((R, Hq), 9.0, device=DEV) if lse else None
+    J.jet_qcache_attention(p.gpu, i64(p.slot0), i32(lens), q, o[:R], row_offsets=i32(offsets(rows)), causal=causal,
+                           scale=scale, lse=ls, **kw)
+    torch.cuda.synchronize()
+    assert torch.all(o[R:] == 9.0)
+    got, qd = o.double().cpu().numpy(), q.double().cpu().numpy()
+    got_l = ls.double().cpu().numpy() if lse else None
+    worst, r = 0.0, 0
+    for s, (n, m) in enumerate(zip(lens, rows)):
+        for h in range(p.H):
+            k, v = p.k[h].values(p.slot0[s], n), p.v[h].values(p.slot0[s], n)
+            hs = slice(h * G, h * G + G)
+            want, wl, pv, qk = ref.attention(qd[r:r + m, hs], k, v, scale, n - m, causal)
+            g = got[r:r + m, hs]
+            ds = (hd + 6) * U * abs(scale) * qk[..., None]
+            big = np.nanmax(np.abs(v)) if n else 0.0
+            tol = pv * (2 * np.expm1(np.minimum(ds, 1.0)) + (n + 64) * U + 2.0 ** -11) + n * 2.0 ** -40 * big * 2
+            tol = tol + np.abs(want) * 1.01 * ref.half_step(otype) + torch.finfo(otype).tiny * ref.half_step(otype) * 2
+            bad = np.isnan(want)
+            np.testing.assert_array_equal(np.isnan(g), bad)
+            err = np.abs(np.where(bad, 0, g - want))
+            assert np.all(err <= np.where(bad, 0, tol)), (s, h, np.nanmax(err / tol))
+            worst = max(worst, float(np.nanmax(np.where(bad, 0, err) / tol, initial=0.0)))
+            if lse:
+                gl, ok = got_l[r:r + m, hs], np.isfinite(wl)
+                np.testing.assert_array_equal(np.isneginf(gl), np.isneginf(wl))
+                np.testing.assert_array_equal(np.isnan(gl), np.isnan(wl))
+                ltol = ds[..., 0] + (n + 64) * U + 4 * U * np.abs(np.where(ok, wl, 0))
+                assert np.all(np.abs(gl[ok] - wl[ok]) <= ltol[ok])
+        r += m
+    assert np.all(got[r:R] == 9.0)
+    return worst
+
+
+def case(seed, fmt, block, hd, H, G, lens, rows, qtype, spread=1.0, gap=0):
+    rng = np.random.default_rng(seed)
+    p = Pair(list(lens), H, hd, block, fmt, gap=gap, extra=1)
+    p.fill(rng, "f32", spread)
+    q = torch.tensor(values(rng, (sum(rows), H * G, hd), 0.3)).to(TORCH[qtype]).to(DEV)
+    return p, q
+
+
+LENS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 500, 1031]
+
+
+@pytest.mark.parametrize("fmt,block,hd,H,G,qtype", [
+    (0, 32, 128, 2, 6, "f16"), (0, 16, 128, 1, 5, "bf16"), (1, 64, 128, 2, 8, "bf16"), (1, 32, 64, 2, 4, "f16"),
+    (0, 128, 64, 1, 1, "f16"), (0, 32, 256, 1, 4, "bf16"), (1, 128, 256, 2, 2, "f16"), (0, 64, 128, 1, 16, "f16"),
+    (1, 16, 128, 1, 24, "f16"), (0, 32, 64, 1, 64, "bf16")])
+def test_one_token_of_each_sequence(fmt, block, hd, H, G, qtype):
+    p, q = case(10, fmt, block, hd, H, G, LENS, [1] * len(LENS), qtype)
+    w = check_attention(p, q, [1] * len(LENS), True)
+    log(f"[ops] one token fmt={fmt} block={block} hd={hd} G={G} {qtype}: {w:.3f} of the tolerance")
+
+
+@pytest.mark.parametrize("fmt,block,hd,H,G,qtype", [
+    (0, 32, 128, 2, 6, "f16"), (1, 16, 128, 1, 5, "bf16"), (0, 64, 64, 1, 1, "bf16"), (1, 128, 256, 1, 3, "f16"),
+    (0, 16, 256, 1, 2, "bf16"), (1, 32, 64, 2, 8, "f16")])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_of_every_count(fmt, block, hd, H, G, qtype, causal):
+    """Ragged rows, among them none, more than the tokens (rows without a key), and all of a sequence."""
+    lens = [1, 40, 33, 130, 64, 300, 5, 0, 77, 260]
+    rows = [1, 3, 33, 130, 0, 17, 9, 2, 70, 129]
+    p, q = case(11, fmt, block, hd, H, G, lens, rows, qtype, gap=1)
+    w = check_attention(p, q, rows, causal)
+    log(f"[ops] rows fmt={fmt} block={block} hd={hd} G={G} {qtype} causal={causal}: {w:.3f} of the tolerance")
+
+
+@pytest.mark.parametrize("qtype,fmt", [("f16", 0), ("bf16", 1)])
+def test_few_sequences_of_many_tokens(qtype, fmt):
+    """Long sequences alone (their keys are split), with few and with many rows."""
+    p, q = case(12, fmt, 32, 128, 2, 5, [9001], [1], qtype)
+    check_attention(p, q, [1], True)
+    check_attention(p, q, [1], True, out="f32")
+    check_attention(p, q, [1], True, lens=[4097])
+    q = torch.cat([q] * 3)
+    check_attention(p, q, [3], True, out="f32")
+    check_attention(p, q, [3], False)
+    q = torch.cat([q] * 14)
+    check_attention(p, q, [42], True, out="f32")
+
+
+def test_outputs_of_32_bits_and_scales():
+    p, q = case(13, 0, 32, 128, 2, 4, [70, 700], [1, 1], "f16")
+    for scale in (0.0, 1.0, -0.125, 1e-3, 20.0):
+        check_attention(p, q, [1, 1], True, out="f32", scale=scale)
+    check_attention(p, q, [1, 1], True, lse=False)
+
+
+@pytest.mark.parametrize("qtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_scales_far_apart(qtype, rows):
+    """Tokens whose scales lie 2^60 apart (a first token of tiny values, later large ones), tiny and huge queries."""
+    rng = np.random.default_rng(14)
+    n = 260
+    p = Pair([n], 1, 128, 16, 0)
+    x = values(rng, (n, 1, 128), 0.1)
+    f = np.exp2(np.repeat([-50, 3, -20, 9, -8, 0, 0, -60, 10, -3, 2, 1, 0, 0, -30, 4, 1], 16)[:n])[:, None, None]
+    k = torch.tensor(x * np.minimum(f, 4.0)).float().to(DEV)
+    v = torch.tensor(values(rng, (n, 1, 128), 0.1) * f).float().to(DEV)
+    p.write([0], k, v, [n])
+    q = torch.tensor(values(rng, (rows, 2, 128), 0.2)).to(TORCH[qtype]).to(DEV)
+    check_attention(p, q, [rows], True, out="f32")
+    if qtype == "bf16":
+        check_attention(p, q * 2.0 ** -80, [rows], True, out="f32", scale=2.0 ** 77)
+        check_attention(p, q * 2.0 ** 60, [rows], True, out="f32", scale=2.0 ** -63)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 50])
+def test_blocks_that_are_not_finite(rows):
+    """A poisoned block makes the rows that see it NaN, and no others; a NaN query spoils its own row only."""
+    rng = np.random.default_rng(15)
+    n = 150
+    p = Pair([n, 60], 1, 64, 16, 0)
+    k, v = (torch.tensor(values(rng, (n + 60, 1, 64))).float().to(DEV) for _ in "kv")
+    v[n - 2, 0, 5] = float("inf")  # in the last block of sequence 0
+    p.write([0, 0], k, v, [n, 60])
+    q = torch.tensor(values(rng, (2 * rows, 2, 64), 0.3)).half().to(DEV)
+    check_attention(p, q, [rows, rows], True)
+    check_attention(p, q, [rows, rows], True, lens=[144, 60])  # up to the block before it
+    k[n + 3, 0, 0] = float("nan")
+    p.write([0, 0], k, v, [n, 60])
+    check_attention(p, q, [rows, rows], True)
+    p = Pair([n, 60], 1, 64, 16, 0)
+    p.fill(rng)
+    q[0, 0, 0], q[rows, 1, 3] = float("nan"), float("inf")
+    check_attention(p, q, [rows, rows], True)
+
+
+def test_strided_queries_and_outputs():
+    p, q = case(16, 0, 32, 128, 2, 3, [50, 90], [4, 1], "f16")
+    big = torch.zeros((7, 12, 130), dtype=torch.float16, device=DEV)
+    big[1:6, ::2, 1:129] = q
+    a = big[1:6, ::2, 1:129]
+    check_attention(p, a, [4, 1], True)
+    want, out = torch.empty_like(q), torch.full((5, 8, 131), 4.0, dtype=torch.float16, device=DEV)
+    J.jet_qcache_attention(p.gpu, i64(p.slot0), i32(p.lens), q, want, row_offsets=i32([0, 4, 5]))
+    J.jet_qcache_attention(p.gpu, i64(p.slot0), i32(p.lens), a, out[:, 1:7, 2:130], row_offsets=i32([0, 4, 5]))
+    assert torch.equal(out[:, 1:7, 2:130], want)
+    out[:, 1:7, 2:130] = 4.0
+    assert torch.all(out == 4.0)
+
+
+def test_same_call_same_bits_and_separate_streams():
+    """Twice the same bits; two calls at once on streams of their own, each with its workspace."""
+    p, q = case(17, 0, 32, 128, 2, 6, [3000, 40, 900], [1, 1, 1], "f16")
+    args = (p.gpu, i64(p.slot0), i32(p.lens), q)
+    a = J.jet_qcache_attention(*args, torch.empty_like(q))
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = []
+    for st in (s1, s2, s1, s2):
+        with torch.cuda.stream(st):
+            outs.append(J.jet_qcache_attention(*args, torch.empty_like(q)))
+    b = J.jet_qcache_attention(*args, torch.empty_like(q), stream=s1.cuda_stream)
+    torch.cuda.synchronize()
+    for o in outs + [b]:
+        assert torch.equal(o, a)
+
+
+def test_cache_past_32_bit_offsets():
+    """Tokens behind 2^32 bytes of a head's values."""
+    H, hd, block = 2, 256, 128
+    slots = (2 ** 32 // hd // block + 40) * block
+    c = J.QCache.empty(H, slots, hd, block)
+    rng = np.random.default_rng(18)
+    n, at = 300, slots - 384
+    k, v = (torch.tensor(values(rng, (n, H, hd))).half().to(DEV) for _ in "kv")
+    J.jet_qcache_write(c, i64([at]), i32([n]), k, v, row_offsets=i32([0, n]))
+    p = Pair([n], H, hd, block, 0)
+    p.write([0], k, v, [n])
+    a, b = torch.empty((n, H, hd), device=DEV), torch.empty((n, H, hd), device=DEV)
+    J.jet_qcache_read(c, i64([at]), i32([n]), a, b, row_offsets=i32([0, n]))
+    for h in range(H):
+        np.testing.assert_array_equal(b[:, h].double().cpu().numpy(), p.v[h].values(0, n))
+    for rows in (1, 100):
+        q = torch.tensor(values(rng, (rows, 4, hd), 0.2)).half().to(DEV)
+        want, got = torch.empty_like(q), torch.empty_like(q)
+        J.jet_qcache_attention(p.gpu, i64([0]), i32([n]), q, want, row_offsets=i32([0, rows]), max_len=n)
+        J.jet_qcache_attention(c, i64([at]), i32([n]), q, got, row_offsets=i32([0, rows]), max_len=n)
+        assert torch.equal(got, want)
+
+
+def test_binding_refuses_what_the_kernels_cannot_take():
+    p, q = case(19, 0, 32, 128, 2, 2, [40], [1], "f16")
+    s0, ln, o = i64(p.slot0), i32(p.lens), torch.empty((1, 4, 128), dtype=torch.float16, device=DEV)
+    k = torch.zeros((1, 2, 128), dtype=torch.float16, device=DEV)
+    for f in (lambda: J.jet_qcache_attention(p.gpu, s0.cpu(), ln, q, o),
+              lambda: J.jet_qcache_attention(p.gpu, s0, ln.long(), q, o),
+              lambda: J.jet_qcache_attention(p.gpu, s0, ln, q.cpu(), o),
+              lambda: J.jet_qcache_attention(p.gpu, s0, ln, q.transpose(1, 2), o.transpose(1, 2)),
+              lambda: J.jet_qcache_attention(p.gpu, s0, ln, q, o[:, :, :64]),
+              lambda: J.jet_qcache_attention(p.gpu, s0, ln, q, o, lse=torch.zeros(3, device=DEV)),
+              lambda: J.jet_qcache_write(p.gpu, s0, ln, k[:, :1], k),
+              lambda: J.jet_qcache_write(p.gpu, s0, ln, k.double(), k),
+              lambda: J.jet_qcache_write(p.gpu, s0, ln, k, k, row_offsets=i32([0])),
+              lambda: J.QCache(p.kb, p.vb[:, :-1], p.ke, p.ve),
+              lambda: J.QCache(p.kb.cpu(), p.vb, p.ke, p.ve),
+              lambda: J.QCache(p.kb, p.vb, p.ke[:, :-1], p.ve)):
+        with pytest.raises((TypeError, ValueError)):
+            f()
+    # host memory where the C ABI expects the cache
+    import ctypes
+    buf = torch.zeros(64 * 128 * 2, dtype=torch.uint8, pin_memory=True)
+    c = J.jet_qcache(0, 32, 2, 128, 64, buf.data_ptr(), buf.data_ptr(), buf.data_ptr(), buf.data_ptr())
+    b = J.jet_qcache_batch(1, 1, 1, 0, 40, s0.data_ptr(), ln.data_ptr(), None)
+    r = J.jet_rows(k.data_ptr(), J.JET_T_F16, 0, 256, 128)
+    assert J.lib().jet_qcache_write(ctypes.byref(c), ctypes.byref(b), ctypes.byref(r), ctypes.byref(r),
+                                    None) == J.JET_E_INVALID
+
+
+# ---------------------------------------------------------------------------
+# logits
+# ---------------------------------------------------------------------------
+
+def logits_case(rng, R, V, dtype, hist, bias, masks, pad=0, neg=True):
+    z = torch.tensor(rng.normal(size=(R, V + pad)) * 5).to(TORCH[dtype]).to(DEV)[:, :V]
+    kw = {}
+    hs = [list(rng.integers(0, max(1, V // 3), size=int(rng.integers(0, hist + 1)))) for _ in range(R)] if hist else []
+    if hist:
+        if V > 2:
+            hs[0] = hs[0] + [V - 1, V - 1, V, -1, 2 ** 31 - 1, V - 2]  # ids outside the vocabulary are ignored
+        kw["history"] = (i32(offsets([len(h) for h in hs])), i32(x for h in hs for x in h))
+        kw["hist_prompt"] = i32(len(h) // 3 for h in hs)
+    bs = [[(int(v), float(np.float32(x))) for v, x in zip(rng.integers(-1, V + 1, size=n), rng.normal(size=n) * 3)]
+          for n in rng.integers(0, bias + 1, size=R)] if bias else []
+    if bias:
+        bs[0] = bs[0] + [(0, 1.0), (0, 1e-9), (0, -1.0), (V - 1, 2.0)] * 3  # the same token again and again
+        kw["bias"] = (i32(offsets([len(b) for b in bs])), i32(v for b in bs for v, _ in b),
+                      torch.tensor([x for b in bs for _, x in b], dtype=torch.float32, device=DEV))
+    allow, idx = None, None
+    if masks:
+        W = (V + 31) // 32
+        allow = rng.random((masks, W * 32)) < rng.random((masks, 1))
+        allow[0] = False  # a state that allows nothing
+        words = np.packbits(allow, axis=1, bitorder="little").view(np.int32)
+        kw["masks"] = torch.tensor(words.copy()).to(DEV)
+        idx = [int(x) for x in rng.integers(-1, masks + 1, size=R)]
+        idx[0] = 0
+        kw["mask_index"] = i32(idx)
+    f = lambda lo, hi: torch.tensor(rng.uniform(lo, hi, size=R), dtype=torch.float32, device=DEV)  # noqa: E731
+    kw.update(repetition=f(0.5, 2.0), presence=f(-1.0, 1.0), frequency=f(-0.5, 0.5))
+    return z, kw, hs, bs, allow, idx
+
+
+def check_logits(z, kw, hs, bs, allow, idx, inplace=False):
+    """Each of at most 4 + len(biases) operations in 32 bits rounds relative to the largest magnitude met, then the type's half step."""
+    R, V = z.shape
+    src = z.double().cpu().numpy()
+    if inplace:
+        got = J.jet_logits_adjust(z, **kw)
+        assert got is z
+    else:
+        full = torch.full((R, V + 3), 6.0, dtype=z.dtype, device=DEV)
+        J.jet_logits_adjust(z, full[:, 1:V + 1], **kw)
+        assert torch.all(full[:, 0] == 6.0) and torch.all(full[:, V + 1:] == 6.0)
+        got = full[:, 1:V + 1]
+        np.testing.assert_array_equal(z.double().cpu().numpy(), src)
+    got = got.double().cpu().numpy()
+    one = lambda k, r, d: d if kw.get(k) is None else float(kw[k][r])  # noqa: E731
+    for r in range(R):
+        al = None
+        if allow is not None and idx[r] >= 0:
+            al = allow[idx[r], :V] if idx[r] < len(allow) else np.zeros(V, bool)
+        h, b = (hs[r] if hs else []), (bs[r] if bs else [])
+        prompt = int(one("hist_prompt", r, 0))
+        want, big = ref.adjust(src[r], h, prompt, one("repetition", r, 1.0), one("presence", r, 0.0),
+                               one("frequency", r, 0.0), b, al)
+        tol = (4 + len(b)) * U * big + ref.half_step(z.dtype) * np.abs(np.where(np.isfinite(want), want, 0)) * 1.01
+        tol += torch.finfo(z.dtype).tiny * ref.half_step(z.dtype) * 2
+        fin = np.isfinite(want)
+        np.testing.assert_array_equal(got[r][~fin], want[~fin])
+        assert np.all(np.abs(got[r][fin] - want[fin]) <= tol[fin]), (r, np.abs(got[r] - want)[fin].max())
+        touched = {v for v in h if 0 <= v < V} | {v for v, _ in b if 0 <= v < V}
+        rest = np.array(sorted(set(range(V)) - touched), int) if V <= 5000 else np.array([], int)
+        rest = rest[al[rest]] if al is not None and len(rest) else rest
+        np.testing.assert_array_equal(got[r][rest], src[r][rest])  # all others pass as they are
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("R,V,hist,bias,masks,pad", [
+    (1, 1, 4, 2, 2, 0), (3, 31, 20, 5, 3, 1), (2, 4095, 60, 0, 2, 0), (4, 4096, 0, 40, 0, 0), (3, 4097, 900, 30, 2, 3),
+    (2, 3000, 60, 600, 3, 8), (5, 20011, 5000, 100, 4, 5), (2, 32768, 0, 0, 2, 0), (2, 151936, 50, 300, 2, 64)])
+def test_logits_rules(dtype, R, V, hist, bias, masks, pad):
+    rng = np.random.default_rng(20)
+    c = logits_case(rng, R, V, dtype, hist, bias, masks, pad)
+    check_logits(*c)
+    check_logits(*c, inplace=True)
+
+
+def test_logits_without_some_rules():
+    rng = np.random.default_rng(21)
+    z, kw, hs, bs, allow, idx = logits_case(rng, 3, 5000, "f32", 40, 10, 3)
+    for drop in (("repetition",), ("presence", "frequency"), ("hist_prompt",), ("repetition", "presence", "frequency")):
+        check_logits(z, {k: v for k, v in kw.items() if k not in drop}, hs, bs, allow, idx)
+    check_logits(z, {}, [], [], None, None)  # none at all: a copy
+    kw.pop("mask_index")
+    check_logits(z, kw, hs, bs, allow, [0, 1, 2])  # mask r for row r
+
+
+def test_logits_that_are_not_numbers():
+    """Infinities and NaN: kept where allowed, -inf where masked."""
+    V = 100
+    z = torch.zeros((1, V), device=DEV)
+    vals = [float("nan"), float("inf"), -float("inf"), torch.finfo(torch.float32).min, 0.0, -0.0]
+    for i, x in enumerate(vals):
+        z[0, i], z[0, 50 + i] = x, x
+    allow = np.ones((1, 128), bool)
+    allow[0, 50:60] = False
+    masks = torch.tensor(np.packbits(allow, axis=1, bitorder="little").view(np.int32).copy()).to(DEV)
+    ids = i32(list(range(6)) + [50, 51, 52])
+    one = lambda x: torch.tensor([x], device=DEV)  # noqa: E731
+    out = J.jet_logits_adjust(z, torch.empty_like(z), history=(i32([0, 9]), ids), repetition=one(2.0),
+                              presence=one(1.0), frequency=one(0.5), masks=masks).cpu()[0]
+    assert torch.isnan(out[0]) and out[1] == float("inf") and out[2] == -float("inf") and out[3] == -float("inf")
+    assert out[4] == -1.5 and out[5] == -1.5 and torch.all(out[50:60] == -float("inf")) and torch.all(out[6:50] == 0)
+
+
+def test_logits_offsets_outside_their_lists():
+    """Offsets that leave their list: the row has no history (no biases)."""
+    z = torch.randn((3, 300), device=DEV)
+    two = torch.full((3,), 2.0, device=DEV)
+    out = J.jet_logits_adjust(z, torch.empty_like(z), history=(i32([0, 5, 3, 900]), i32([1, 2, 3, 4, 5])),
+                              repetition=two, bias=(i32([-1, 2, 1, 7]), i32([1, 2, 3]), torch.ones(3, device=DEV)))
+    want = z.clone()
+    want[0, 1:6] = torch.where(z[0, 1:6] > 0, z[0, 1:6] / 2, z[0, 1:6] * 2)
+    assert torch.equal(out, want)
+
+
+def test_logits_of_many_rows():
+    """More rows than one launch's grid, short vocabularies."""
+    R, V = 70000, 5
+    z = torch.randn((R, V), device=DEV)
+    ids = torch.arange(R, dtype=torch.int32, device=DEV) % V
+    out = J.jet_logits_adjust(z, torch.empty_like(z), history=(torch.arange(R + 1, dtype=torch.int32, device=DEV), ids),
+                              frequency=torch.arange(R, dtype=torch.float32, device=DEV))
+    want = z.clone()
+    want[torch.arange(R, device=DEV), ids.long()] -= torch.arange(R, dtype=torch.float32, device=DEV)
+    assert torch.equal(out, want)
+
+
+# ---------------------------------------------------------------------------
+# together, as a decode step uses them
+# ---------------------------------------------------------------------------
+
+def test_decode_steps_captured_and_replayed():
+    """Append, attend and adjust as one captured graph whose lengths and inputs live on the device, replayed with
+    eager work between, against the same steps made eagerly on a second cache."""
+    rng = np.random.default_rng(30)
+    H, G, hd, block, n_seq, V = 2, 3, 128, 16, 3, 700
+    lens = [30, 47, 5]
+    steps = 40
+    slots = [0, 96, 192]
+    caches = [J.QCache.empty(H, 288, hd, block) for _ in range(2)]
+    k0, v0 = (torch.tensor(values(rng, (sum(lens), H, hd))).half().to(DEV) for _ in "kv")
+    for c in caches:
+        J.jet_qcache_write(c, i64(slots), i32(lens), k0, v0, row_offsets=i32(offsets(lens)))
+    slot0, ln = i64(slots), i32(lens)
+    K, Vv = (torch.tensor(values(rng, (steps, n_seq, H, hd))).half().to(DEV) for _ in "kv")
+    Q = torch.tensor(values(rng, (steps, n_seq, H * G, hd), 0.2)).half().to(DEV)
+    Z = torch.randn((steps, n_seq, V), device=DEV)
+    hist = i32([x % 50 for x in range(60)])
+    hoff, rep = i32([0, 20, 40, 60]), torch.full((n_seq,), 1.2, device=DEV)
+    k, v, q, z = K[0].clone(), Vv[0].clone(), Q[0].clone(), Z[0].clone()
+    out, zo = torch.empty_like(q), torch.empty_like(z)
+    ws = torch.empty(J.jet_qcache_attention_workspace(caches[0], n_seq, H * G), dtype=torch.uint8, device=DEV)
+
+    def step(c, ln, k, v, q, out, z, zo, ws):
+        J.jet_qcache_write(c, slot0, ln, k, v)
+        J.jet_qcache_attention(c, slot0, ln, q, out, workspace=ws)
+        J.jet_logits_adjust(z, zo, history=(hoff, hist), repetition=rep)
+
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    ln.zero_()  # the captured call itself must not matter
+    with torch.cuda.graph(g, stream=st):
+        step(caches[0], ln, k, v, q, out, z, zo, ws)
+    for t in range(steps):
+        ln.copy_(i32([n + t + 1 for n in lens]))
+        k.copy_(K[t]), v.copy_(Vv[t]), q.copy_(Q[t]), z.copy_(Z[t])
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        o2, z2 = torch.empty_like(q), torch.empty_like(z)
+        step(caches[1], i32([n + t + 1 for n in lens]), K[t], Vv[t], Q[t], o2, Z[t], z2, torch.empty_like(ws))
+        assert torch.equal(out, o2) and torch.equal(zo, z2), t
+    for a, b in zip(caches[0].tensors, caches[1].tensors):
+        full = [n + steps for n in lens]
+        r = [[torch.empty((sum(full), H, hd), device=DEV) for _ in "kv"] for _ in caches]
+        for c, x in zip(caches, r):
+            J.jet_qcache_read(c, slot0, i32(full), x[0], x[1], row_offsets=i32(offsets(full)))
+        assert torch.equal(r[0][0], r[1][0]) and torch.equal(r[0][1], r[1][1])
