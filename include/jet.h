@@ -389,8 +389,8 @@ const char *jet_last_error(void);
  * What the host can see (NULL, counts, types, alignment) is refused with
  * JET_E_INVALID before anything is enqueued. What lies in device memory cannot
  * be refused: kernels check it against the counts given here, and a sequence
- * or row that lies outside of them is left out (nothing is read or written
- * for it; attention gives it zeros).
+ * or row that lies outside of them is left out: nothing is read or written
+ * for it.
  * ---------------------------------------------------------------------------
  */
 

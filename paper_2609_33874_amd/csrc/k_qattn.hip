@@ -2,66 +2,385 @@
 //
 // For row i of a sequence and query head h over KV head h / G:
 //   s_j = scale 2^(ek_j) sum_d q_d k_jd,  o = sum_j softmax(s)_j 2^(ev_j) v_j
-// over the tokens j that the row sees, with the running maximum and sum of the
-// softmax kept as the keys pass.
+// over the tokens j that the row sees, in one pass with the running maximum and
+// sum of the softmax. The 8-bit values are exact in f16, so both products run
+// on the matrix cores in f16 with the scales outside of them: K's on the
+// scores, V's on the probabilities. A probability goes into the second product
+// as p 2^(ev - M) 2^15 in f16, M the largest V exponent met so far (the
+// accumulators are in units of 2^(M - 15) and rescaled when M grows), so that
+// what it loses is its rounding to 11 bits, or 2^-40 of the largest value.
+// bf16 queries enter as f16 times a power of two that puts a row's largest
+// value in [2^14, 2^15): exact down to 2^-30 of it.
 #include <algorithm>
 
 #include "qcache.h"
 
 namespace jetk {
 
-int64_t qattn_workspace(const QCache &, const QBatch &, int) { return 0; }
+// ---------------------------------------------------------------------------
+// Few query rows: keys split over waves and workgroups
+// ---------------------------------------------------------------------------
 
-// One wave per (row, query head); lane l holds dims l D .. l D + D - 1.
-template <typename T, typename O, int FMT, int D>
-__global__ __launch_bounds__(64) void qattn_row_kernel(QAttn a) {
-  const int lane = threadIdx.x, hq = blockIdx.y, h = hq / (a.Hq / a.c.H);
-  const QSeq s = qseq(a.b, a.c, blockIdx.z);
-  const int hd = a.c.hd;
-  const uint8_t *k = a.c.k + ((int64_t)h * a.c.S + s.slot0) * hd + lane * D;
-  const uint8_t *v = a.c.v + ((int64_t)h * a.c.S + s.slot0) * hd + lane * D;
-  const uint8_t *ke = a.c.ke + (int64_t)h * (a.c.S >> a.c.lb) + (s.slot0 >> a.c.lb);
-  const uint8_t *ve = a.c.ve + (int64_t)h * (a.c.S >> a.c.lb) + (s.slot0 >> a.c.lb);
-  auto scale_of = [](int e) { return e == kExpNaN ? __uint_as_float(0x7fc00000u) : pow2i(e - kExpBias); };
-  for (int i = blockIdx.x; i < s.n; i += gridDim.x) {
-    const int64_t row = s.row0 + i;
-    const int pos = s.pos0 + i, end = pos < 0 ? 0 : a.causal ? pos + 1 : s.len;
-    const T *q = (const T *)a.q.p + row * a.q.rs + (int64_t)hq * a.q.hs + lane * D;
-    float x[D], o[D], m = -INFINITY, l = 0.0f;
+constexpr int kTile = 32;    // keys of a wave's step
+constexpr int kWaves = 4;    // waves of a workgroup, on neighbouring tiles
+constexpr int kMaxSplit = 128;
+
+template <int HD> struct QTile {
+  static constexpr int KW = HD / 16;  // 32-bit words of K per lane and 16 keys
+  static constexpr int VW = HD / 64;  // of V per lane and key
+  uint32_t k[2][KW], v[8][VW];
+  int ke[2], ve[2];
+};
+
+// Words of a row into registers: N words from p (aligned to their size).
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t *p) {
+  if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t *>(p);
+  } else if constexpr (N == 2) {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    w[0] = u.x; w[1] = u.y;
+  } else {
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      x[d] = to_f<T>(q[d]);
-      o[d] = 0.0f;
+    for (int i = 0; i < N / 4; ++i) {
+      const uint4 u = ld16(p + 16 * i);
+      w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
     }
-    for (int j = 0; j < end; ++j) {
-      float dot = 0.0f;
-#pragma unroll
-      for (int d = 0; d < D; ++d) dot += x[d] * unpack8<FMT, 0>(k[(int64_t)j * hd + d]);
-      const float z = warp_sum(dot) * scale_of(ke[j >> a.c.lb]) * a.scale * kLog2e;
-      const float top = fmaxf(m, z);
-      const float base = top == -INFINITY ? 0.0f : top;
-      const float f = __builtin_amdgcn_exp2f(m - base), p = __builtin_amdgcn_exp2f(z - base);
-      l = l * f + p;
-      const float pv = p * scale_of(ve[j >> a.c.lb]);
-#pragma unroll
-      for (int d = 0; d < D; ++d) o[d] = o[d] * f + pv * unpack8<FMT, 0>(v[(int64_t)j * hd + d]);
-      m = top;
-    }
-    const float inv = end > 0 ? 1.0f / l : 0.0f;
-    O *out = (O *)a.out.p + row * a.out.rs + (int64_t)hq * a.out.hs + lane * D;
-#pragma unroll
-    for (int d = 0; d < D; ++d) out[d] = from_f<O>(o[d] * inv);
-    if (a.lse && lane == 0) a.lse[row * a.Hq + hq] = end > 0 ? m * kLn2 + logf(l) : -INFINITY;
   }
+}
+
+// Partial results of a split: o [split][row * Hq + head][hd] (not divided by
+// l), then m and l [split][row * Hq + head].
+struct Parts {
+  float *o, *m, *l;
+};
+__device__ __host__ __forceinline__ Parts parts_of(void *ws, int64_t n, int nsplit, int hd) {
+  float *o = (float *)ws;
+  return {o, o + n * nsplit * hd, o + n * nsplit * (hd + 1)};
+}
+
+// One workgroup per (block of 16 QB query slots and split of the keys, KV
+// head, sequence); slot = row * G + head. Each wave takes every fourth tile of
+// 32 keys of the split on its own (K and V go straight into registers as the
+// matrix cores take them, the next tile's on their way meanwhile), and the
+// waves' results are joined in LDS.
+// A lane (g = lane / 16, c = lane % 16) holds of K dims HD/4 g .. of key c, as
+// the A operand of S^T = K Q^T; then for query c the scores of keys 4 g .. + 3,
+// as the B operand of O^T = V^T P^T; and of V the HD/16 dims from HD/16 c of
+// those same keys: a transposition of bytes inside the lane makes the A
+// operand, dim HD/16 c + i in product i.
+template <typename T, typename O, int FMT, int HD, int QB>
+__global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int nsplit) {
+  constexpr int ND = HD / 16, NK = HD / 32, LD = HD + 4;
+  typedef QTile<HD> Tile;
+  __shared__ float s_o[kWaves][16 * QB][LD];
+  __shared__ float s_m[kWaves][16 * QB], s_l[kWaves][16 * QB];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 4, c = lane & 15;
+  const int h = blockIdx.y, G = a.Hq / a.c.H, sp = blockIdx.x % nsplit;
+  const QSeq sq = qseq(a.b, a.c, blockIdx.z);
+  const int slots = sq.n * G;
+  const int64_t base = ((int64_t)h * a.c.S + sq.slot0) * HD;
+  const uint8_t *K = a.c.k + base, *V = a.c.v + base;
+  const int64_t ebase = (int64_t)h * (a.c.S >> a.c.lb) + (sq.slot0 >> a.c.lb);
+  const uint8_t *KE = a.c.ke + ebase, *VE = a.c.ve + ebase;
+
+  for (int sb = blockIdx.x / nsplit * 16 * QB; sb < slots; sb += gridDim.x / nsplit * 16 * QB) {
+    // keys of this block: up to the last one that its last row sees
+    const int last_row = (min(sb + 16 * QB, slots) - 1) / G;
+    const int kend = max(0, a.causal ? sq.pos0 + last_row + 1 : sq.len);
+    const int ntile = (kend + kTile - 1) / kTile, per = (ntile + nsplit - 1) / nsplit;
+    const int t1 = min(ntile, (sp + 1) * per);
+    int t = sp * per + wave;
+
+    int vis[QB], vis_min = kend;  // keys that this lane's queries see
+    Frag<f16> qf[QB][NK];
+    float fq[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int slot = sb + qb * 16 + c, i = min(slot, slots - 1) / G, head = h * G + min(slot, slots - 1) % G;
+      const int pos = sq.pos0 + i;
+      vis[qb] = pos < 0 ? 0 : a.causal ? pos + 1 : sq.len;
+      vis_min = min(vis_min, vis[qb]);
+      const T *q = (const T *)a.q.p + (int64_t)(sq.row0 + i) * a.q.rs + (int64_t)head * a.q.hs + g * (HD / 4);
+      float x[NK][8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        if (a.q.vec) {
+          const uint4 u = ld16(q + ks * 8);
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[ks][2 * j] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] & 0xffff)));
+            x[ks][2 * j + 1] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] >> 16)));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[ks][j] = to_f<T>(q[ks * 8 + j]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[ks][j]) & 0x7fffffffu);
+      }
+      float up = 1.0f;
+      fq[qb] = a.scale * kLog2e;
+      if constexpr (sizeof(T) == 2 && !__is_same(T, f16)) {
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        // largest value 2^x f, f in [1, 2): times 2^(14 - x), and back on the scores
+        const int e = min(max((int)(top >> 23) - 127, -112), 127);
+        if (top) up = pow2i(14 - e);
+        if (top) fq[qb] *= pow2i(e - 14);
+      }
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[qb][ks].v[j] = (f16)(x[ks][j] * up);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) vis_min = min(vis_min, __shfl_xor(vis_min, o));
+
+    auto load = [&](Tile &x, int tile) {
+      const int k0 = tile * kTile, last = sq.len - 1;  // keys past the end load the last one (they are masked)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const int64_t r = min(k0 + kb * 16 + c, last);
+        load_words(x.k[kb], K + r * HD + g * (HD / 4));
+        const int b = min(k0 + kb * 16, last) >> a.c.lb;
+        x.ke[kb] = KE[b];
+        x.ve[kb] = VE[b];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t r = min(k0 + (i >> 2) * 16 + 4 * g + (i & 3), last);
+        load_words(x.v[i], V + r * HD + c * ND);
+      }
+    };
+
+    float m[QB], l[QB];
+    f32x4 acc[QB][ND];
+    int M = 0;  // V exponent byte of the accumulators' unit
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      m[qb] = -INFINITY;
+      l[qb] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[qb][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    Tile cur, nxt;
+    if (t < t1) load(cur, t);
+    for (; t < t1; t += kWaves) {
+      if (t + kWaves < t1) load(nxt, t + kWaves);
+      const int k0 = t * kTile;
+      f32x4 s[QB][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+          const uint2 lo = f16x4_of<FMT>(cur.k[kb][2 * ks]), hi = f16x4_of<FMT>(cur.k[kb][2 * ks + 1]);
+          Frag<f16> kf;
+          kf.v = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) mma16(s[qb][kb], kf, qf[qb][ks]);
+        }
+      }
+      const int ke0 = __builtin_amdgcn_readfirstlane(cur.ke[0]), ke1 = __builtin_amdgcn_readfirstlane(cur.ke[1]);
+      const int ve0 = __builtin_amdgcn_readfirstlane(cur.ve[0]), ve1 = __builtin_amdgcn_readfirstlane(cur.ve[1]);
+      const float nan = __uint_as_float(0x7fc00000u);
+      const float ks2[2] = {ke0 == kExpNaN ? nan : pow2i(ke0 - kExpBias), ke1 == kExpNaN ? nan : pow2i(ke1 - kExpBias)};
+      const int Mn = max(M, max(ve0 == kExpNaN ? 0 : ve0, ve1 == kExpNaN ? 0 : ve1));
+      // the tile's V scales in units of 2^(Mn - 15), and the accumulators' old unit in the new one's
+      const float vs[2] = {ve0 == kExpNaN ? nan : ve0 - Mn < -126 ? 0.0f : pow2i(ve0 - Mn + 15),
+                           ve1 == kExpNaN ? nan : ve1 - Mn < -126 ? 0.0f : pow2i(ve1 - Mn + 15)};
+      const float unit = M - Mn < -126 ? 0.0f : pow2i(M - Mn);
+      M = Mn;
+      const bool all_seen = k0 + kTile <= vis_min;
+      Frag<f16> pf[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float z[2][4], mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[kb][e] = s[qb][kb][e] * ks2[kb] * fq[qb];
+            if (!all_seen && k0 + kb * 16 + 4 * g + e >= vis[qb]) z[kb][e] = -INFINITY;
+            mx = fmaxf(mx, z[kb][e]);
+          }
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = fmaxf(m[qb], mx), ms = mn == -INFINITY ? 0.0f : mn;
+        const float alpha = __builtin_amdgcn_exp2f(m[qb] - ms);
+        m[qb] = mn;
+        float p[2][4], sum = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[kb][e] = __builtin_amdgcn_exp2f(z[kb][e] - ms);
+            sum += p[kb][e];
+            // (a masked key's 0 must stay 0 where the block's scale is NaN)
+            p[kb][e] = z[kb][e] == -INFINITY ? 0.0f : p[kb][e] * vs[kb];
+          }
+        l[qb] = l[qb] * alpha + sum;
+        const float al = alpha * unit;
+        if (__any(al != 1.0f)) {
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc[qb][d] *= al;
+        }
+        const uint4 u = make_uint4(f2h2(p[0][0], p[0][1]), f2h2(p[0][2], p[0][3]), f2h2(p[1][0], p[1][1]),
+                                   f2h2(p[1][2], p[1][3]));
+        pf[qb].v = __builtin_bit_cast(f16x8, u);
+      }
+#pragma unroll
+      for (int w = 0; w < Tile::VW; ++w) {
+        uint32_t a0[4] = {cur.v[0][w], cur.v[1][w], cur.v[2][w], cur.v[3][w]};
+        uint32_t a1[4] = {cur.v[4][w], cur.v[5][w], cur.v[6][w], cur.v[7][w]};
+        transpose4(a0);
+        transpose4(a1);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const uint2 lo = f16x4_of<FMT>(a0[b]), hi = f16x4_of<FMT>(a1[b]);
+          Frag<f16> vf;
+          vf.v = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) mma16(acc[qb][4 * w + b], vf, pf[qb]);
+        }
+      }
+      cur = nxt;
+    }
+
+    // the waves' results in LDS, in units of 1
+    const float up = pow2i(max(M - kExpBias - 15, -126));
+    __syncthreads();  // the last block's have been read
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float lt = l[qb] + __shfl_xor(l[qb], 16);
+      lt += __shfl_xor(lt, 32);
+      const int q = qb * 16 + c;
+      if (g == 0) {
+        s_m[wave][q] = m[qb];
+        s_l[wave][q] = lt;
+      }
+      // acc[i][e] is dim ND (4 g + e) + i
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < ND; i += 4) {
+          const f32x4 o = {acc[qb][i][e] * up, acc[qb][i + 1][e] * up, acc[qb][i + 2][e] * up, acc[qb][i + 3][e] * up};
+          *reinterpret_cast<f32x4 *>(&s_o[wave][q][ND * (4 * g + e) + i]) = o;
+        }
+    }
+    __syncthreads();
+    constexpr int CPQ = HD / 4;  // chunks of 4 dims per query
+    const Parts parts = parts_of(a.ws, (int64_t)a.b.n_rows * a.Hq, nsplit, HD);
+    for (int i = tid; i < 16 * QB * CPQ; i += 64 * kWaves) {
+      const int q = i / CPQ, d = i % CPQ * 4, slot = sb + q;
+      if (slot >= slots) break;
+      float mm = s_m[0][q];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, s_m[w][q]);
+      const float ms = mm == -INFINITY ? 0.0f : mm;
+      float lt = 0.0f;
+      f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w][q] - ms);
+        lt += s_l[w][q] * f;
+        o += *reinterpret_cast<const f32x4 *>(&s_o[w][q][d]) * f;
+      }
+      const int64_t row = sq.row0 + slot / G, head = h * G + slot % G, at = row * a.Hq + head;
+      if (nsplit > 1) {
+        const int64_t n = (int64_t)a.b.n_rows * a.Hq;
+        *reinterpret_cast<f32x4 *>(parts.o + (sp * n + at) * HD + d) = o;
+        if (d == 0) {
+          parts.m[sp * n + at] = mm;
+          parts.l[sp * n + at] = lt;
+        }
+      } else {
+        const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+        O *out = (O *)a.out.p + row * a.out.rs + head * a.out.hs + d;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] = from_f<O>(o[j] * inv);
+        if (a.lse && d == 0) a.lse[at] = lt == 0.0f ? -INFINITY : mm * kLn2 + logf(lt);
+      }
+    }
+  }
+}
+
+// One workgroup per (row of a sequence, query head): the splits' results
+// joined. Rows of no sequence have no results and are left out.
+template <typename O, int HD>
+__global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
+  constexpr int D = HD / 64;
+  __shared__ float s_m[4], s_l[4], s_o[4][HD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.y;
+  const QSeq sq = qseq(a.b, a.c, blockIdx.z);
+  const int64_t n = (int64_t)a.b.n_rows * a.Hq;
+  const Parts parts = parts_of(a.ws, n, nsplit, HD);
+  for (int i = blockIdx.x; i < sq.n; i += gridDim.x) {
+    const int64_t row = sq.row0 + i, at = row * a.Hq + head;
+    // every wave finds the maximum over all splits, then adds up every fourth one
+    float mm = -INFINITY;
+    for (int s = lane; s < nsplit; s += 64) mm = fmaxf(mm, parts.m[s * n + at]);
+    mm = warp_max(mm);
+    const float ms = mm == -INFINITY ? 0.0f : mm;
+    float l = 0.0f, o[D] = {};
+#pragma unroll 8
+    for (int s = wave; s < nsplit; s += 4) {
+      const float f = __builtin_amdgcn_exp2f(parts.m[s * n + at] - ms);
+      l += parts.l[s * n + at] * f;
+      const float *p = parts.o + (s * n + at) * HD + lane * D;
+#pragma unroll
+      for (int d = 0; d < D; ++d) o[d] += p[d] * f;
+    }
+    __syncthreads();
+    if (lane == 0) s_l[wave] = l;
+#pragma unroll
+    for (int d = 0; d < D; ++d) s_o[wave][lane * D + d] = o[d];
+    __syncthreads();
+    if (tid < HD) {
+      const float lt = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+      const float ot = s_o[0][tid] + s_o[1][tid] + s_o[2][tid] + s_o[3][tid];
+      ((O *)a.out.p)[row * a.out.rs + head * a.out.hs + tid] = from_f<O>(lt == 0.0f ? 0.0f : ot / lt);
+      if (a.lse && tid == 0) a.lse[at] = lt == 0.0f ? -INFINITY : mm * kLn2 + logf(lt);
+    }
+  }
+}
+
+// Query slots of a sequence and KV head, and the splits of their keys: enough
+// workgroups for four on each of 256 CUs, of at least two tiles a wave.
+static int64_t slots_of(const QCache &c, const QBatch &b, int Hq) { return (int64_t)std::max(b.max_rows, 1) * (Hq / c.H); }
+static int splits_of(const QCache &c, const QBatch &b, int Hq) {
+  const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots_of(c, b, Hq) + 15) / 16);
+  const int64_t most = std::min<int64_t>((std::max<int64_t>(b.max_len, 1) + 255) / 256, kMaxSplit);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (1024 + units - 1) / units));
+}
+
+int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
+  const int n = splits_of(c, b, Hq);
+  return n == 1 ? 0 : (int64_t)b.n_rows * Hq * n * (c.hd + 2) * 4;
+}
+
+template <typename T, typename O, int FMT, int HD>
+static hipError_t run_split(const QAttn &a, hipStream_t st) {
+  const int nsplit = splits_of(a.c, a.b, a.Hq);
+  const int64_t blocks = std::min<int64_t>((slots_of(a.c, a.b, a.Hq) + 15) / 16, 65536);
+  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)(blocks * nsplit), a.c.H, a.b.n_seq),
+                     dim3(64 * kWaves), 0, st, a, nsplit);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || nsplit == 1) return e;
+  const unsigned rows = (unsigned)std::min(std::max(a.b.max_rows, 1), 65536);
+  hipLaunchKernelGGL((qattn_join_kernel<O, HD>), dim3(rows, a.Hq, a.b.n_seq), dim3(256), 0, st, a, nsplit);
+  return hipGetLastError();
 }
 
 template <typename T, typename O, int FMT>
 static hipError_t run_hd(const QAttn &a, hipStream_t st) {
-  const dim3 grid((unsigned)std::min(std::max(a.b.max_rows, 1), 65536), (unsigned)a.Hq, (unsigned)a.b.n_seq);
-  if (a.c.hd == 64) hipLaunchKernelGGL((qattn_row_kernel<T, O, FMT, 1>), grid, dim3(64), 0, st, a);
-  else if (a.c.hd == 128) hipLaunchKernelGGL((qattn_row_kernel<T, O, FMT, 2>), grid, dim3(64), 0, st, a);
-  else hipLaunchKernelGGL((qattn_row_kernel<T, O, FMT, 4>), grid, dim3(64), 0, st, a);
-  return hipGetLastError();
+  if (a.c.hd == 64) return run_split<T, O, FMT, 64>(a, st);
+  if (a.c.hd == 128) return run_split<T, O, FMT, 128>(a, st);
+  return run_split<T, O, FMT, 256>(a, st);
 }
 template <typename T, typename O> static hipError_t run_fmt(const QAttn &a, hipStream_t st) {
   return a.c.fmt == 0 ? run_hd<T, O, 0>(a, st) : run_hd<T, O, 1>(a, st);

@@ -66,4 +66,29 @@ template <int FMT, int J> __device__ __forceinline__ float unpack8(uint32_t w) {
   return __builtin_amdgcn_cvt_f32_fp8((int)w, J);
 }
 
+// Four bytes of the cache as f16 (exact: int8 has 7 bits and a sign, e4m3 4).
+// int8: byte ^ 0x80 under the exponent of 1024 is 1024 + 128 + q.
+template <int FMT> __device__ __forceinline__ uint2 f16x4_of(uint32_t w) {
+  if (FMT == 0) {
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t lo = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u), hi = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
+    const f16x2_t c = {(f16)1152.0f, (f16)1152.0f};
+    const f16x2_t a = __builtin_bit_cast(f16x2_t, lo) - c, b = __builtin_bit_cast(f16x2_t, hi) - c;
+    return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+  }
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+  const auto b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
+  return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+
+// Bytes of four words transposed: word b of the result holds byte b of each.
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
 }  // namespace jetk
