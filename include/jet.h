@@ -520,13 +520,13 @@ typedef struct {
   const int32_t *hist_offsets;    /* device, [n_rows + 1], or NULL: no history */
   const int32_t *hist_ids;        /* device, [n_hist] */
   const int32_t *hist_prompt;     /* device, [n_rows], or NULL: 0 */
-  int64_t n_hist;                 /* ids in hist_ids (< 2^31) */
+  int64_t n_hist;                 /* ids in hist_ids (<= 2^30) */
   const float *repetition;        /* device, [n_rows], > 0, or NULL: 1 */
   const float *presence, *frequency; /* device, [n_rows], or NULL: 0 */
   const int32_t *bias_offsets;    /* device, [n_rows + 1], or NULL: no biases */
   const int32_t *bias_ids;        /* device, [n_bias] */
   const float *bias_values;       /* device, [n_bias] */
-  int64_t n_bias;                 /* < 2^31 */
+  int64_t n_bias;                 /* <= 2^30 */
   const uint32_t *masks;          /* device, [n_masks][mask_stride], or NULL: bit
                                      v % 32 of word v / 32 allows token v */
   int64_t mask_stride;            /* words, >= ceil(vocab / 32) */

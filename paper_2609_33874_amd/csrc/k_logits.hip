@@ -16,81 +16,229 @@ namespace jetk {
 
 constexpr int kSlice = 4096, kLogitThreads = 256;
 
-template <typename T>
+// The rules of one token. c: bit 0, in the history; the rest, how often behind
+// the prompt. Without branches: where a vector has any token of the lists, all
+// of its tokens go through (a division and a branch each made the kernel bound
+// by instructions), and those of no list come out as they went in.
+struct RowRules {
+  float rep, inv, pres, freq;  // inv = 1 / rep
+};
+__device__ __forceinline__ float adjusted(float z, uint32_t c, float bias, const RowRules &w) {
+  const float f = z > 0.0f ? w.inv : w.rep;
+  z *= c ? f : 1.0f;
+  z -= c > 1 ? w.freq * (float)(c >> 1) + w.pres : 0.0f;
+  return z + bias;
+}
+
+__device__ const int32_t kNone[2] = {0, 0};
+__device__ const float kOne = 1.0f, kZero = 0.0f;
+
+// HIST, BIAS: whether any row may have a history or biases. VEC: rows of in and
+// out start at 16-byte boundaries.
+template <typename T, bool HIST, bool BIAS, bool VEC>
 __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs a) {
-  __shared__ uint32_t cnt[kSlice];  // bit 0: in the history; the rest: how often behind the prompt
-  __shared__ float bias[kSlice];
-  __shared__ int l_id[kLogitThreads];
-  __shared__ float l_val[kLogitThreads];
-  __shared__ int l_n[kLogitThreads / 64];
+  // the slice's counters, then (in the same place: two arrays would halve the
+  // workgroups a CU holds, 72 us for 39 in the case below) its biases
+  __shared__ __align__(16) uint32_t cnt[HIST || BIAS ? kSlice : 4];
+  float *bias = reinterpret_cast<float *>(cnt);
   const int tid = threadIdx.x, r = blockIdx.y, v0 = blockIdx.x * kSlice, nv = min(kSlice, a.V - v0);
-  int h0 = 0, h1 = 0, b0 = 0, b1 = 0;
-  if (a.h_off) {
-    h0 = a.h_off[r];
-    h1 = a.h_off[r + 1];
-    if (h0 < 0 || h1 < h0 || h1 > a.n_hist) h0 = h1 = 0;
-  }
-  if (a.b_off) {
-    b0 = a.b_off[r];
-    b1 = a.b_off[r + 1];
-    if (b0 < 0 || b1 < b0 || b1 > a.n_bias) b0 = b1 = 0;
-  }
-  if (h1 > h0) {
-    for (int i = tid; i < kSlice; i += kLogitThreads) cnt[i] = 0;
-    __syncthreads();
-    const int made = a.h_prompt ? max(0, a.h_prompt[r]) : 0;
-    for (int i = h0 + tid; i < h1; i += kLogitThreads) {
-      const uint32_t v = (uint32_t)a.h_ids[i] - (uint32_t)v0;
-      if (v < (uint32_t)nv) {
-        atomicOr(&cnt[v], 1u);
-        if (i - h0 >= made) atomicAdd(&cnt[v], 2u);
-      }
-    }
-  }
-  if (b1 > b0) {
-    for (int i = tid; i < kSlice; i += kLogitThreads) bias[i] = 0.0f;
-    // a run of the list at a time: its entries inside the slice are kept in
-    // order, then every thread adds those of its own tokens
-    for (int i0 = b0; i0 < b1; i0 += kLogitThreads) {
-      const int i = i0 + tid;
-      const uint32_t v = i < b1 ? (uint32_t)a.b_ids[i] - (uint32_t)v0 : 0xffffffffu;
-      const bool in = v < (uint32_t)nv;
-      const uint64_t m = __ballot(in);
-      if ((tid & 63) == 0) l_n[tid >> 6] = __popcll(m);
-      __syncthreads();
-      int at = __popcll(m & ((1ull << (tid & 63)) - 1)), n = 0;
-      for (int w = 0; w < kLogitThreads / 64; ++w) {
-        if (w < tid >> 6) at += l_n[w];
-        n += l_n[w];
-      }
-      if (in) {
-        l_id[at] = (int)v;
-        l_val[at] = a.b_val[i];
-      }
-      __syncthreads();
-      for (int j = 0; j < n; ++j)
-        if (l_id[j] % kLogitThreads == tid) bias[l_id[j]] += l_val[j];
-      __syncthreads();
-    }
-  }
-  __syncthreads();
-  const int mi = !a.masks ? -1 : a.mask_index ? a.mask_index[r] : r;
-  const uint32_t *mask = mi < 0 ? nullptr : a.masks + (int64_t)mi * a.mask_ld;
-  const float rep = a.rep ? a.rep[r] : 1.0f, pres = a.pres ? a.pres[r] : 0.0f, freq = a.freq ? a.freq[r] : 0.0f;
   const T *in = (const T *)a.in + (int64_t)r * a.in_ld + v0;
   T *out = (T *)a.out + (int64_t)r * a.out_ld + v0;
-  for (int i = tid; i < nv; i += kLogitThreads) {
-    const int v = v0 + i;
-    const bool allowed = !mask || (mi < a.n_masks && (mask[v >> 5] >> (v & 31) & 1));
-    float z = to_f<T>(in[i]);
-    if (h1 > h0) {
-      const uint32_t c = cnt[i];
-      if (c) z = z > 0.0f ? z / rep : z * rep;
-      if (c > 1) z -= freq * (float)(c >> 1) + pres;
+  const bool inplace = a.in == a.out;
+  constexpr int N = VEC ? 16 / sizeof(T) : 1;  // tokens of a vector; they lie in one word of the mask
+  constexpr int NV = kSlice / kLogitThreads / N;
+  // The slice's logits are on their way while the lists are counted (unless
+  // they are changed in place, where most need not be read at all).
+  uint4 u[VEC ? NV : 1];
+  uint32_t m[VEC ? NV : 1];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = (k * kLogitThreads + tid) * N;
+      if (!inplace && i + N <= nv) u[k] = ld16(in + i);
     }
-    if (b1 > b0) z += bias[i];
-    out[i] = from_f<T>(allowed ? z : -INFINITY);
   }
+  // what belongs to the row, in one round of loads: absent rules read a default
+  const int32_t *hp = HIST ? a.h_off + r : kNone, *bp = BIAS ? a.b_off + r : kNone;
+  const int32_t *pp = HIST && a.h_prompt ? a.h_prompt + r : kNone, *ip = a.mask_index ? a.mask_index + r : kNone;
+  const float *rp = a.rep ? a.rep + r : &kOne, *sp = a.pres ? a.pres + r : &kZero, *fp = a.freq ? a.freq + r : &kZero;
+  int h0 = hp[0], h1 = hp[1], b0 = bp[0], b1 = bp[1];
+  const int prompt = pp[0], index = ip[0];
+  const RowRules w = {*rp, 1.0f / *rp, *sp, *fp};
+  if (h0 < 0 || h1 < h0 || h1 > a.n_hist) h0 = h1 = 0;
+  if (b0 < 0 || b1 < b0 || b1 > a.n_bias) b0 = b1 = 0;
+  const int mi = !a.masks ? -1 : a.mask_index ? index : r;
+  const bool none = mi >= a.n_masks;  // a mask that does not exist allows nothing
+  const uint32_t *mask = mi < 0 || none ? nullptr : a.masks + (int64_t)mi * a.mask_ld + v0 / 32;
+  const bool hist = HIST && h1 > h0, biased = BIAS && b1 > b0;
+  // A batch of the history is eight ids a thread, one of the biases four a lane
+  // of the first wave; the first ones are on their way while LDS is cleared. An
+  // id of -1 lies in no slice.
+  const bool adds = biased && tid < 64;
+  int hid[HIST ? 8 : 1], hnext[HIST ? 8 : 1], bid[BIAS ? 4 : 1];
+  float bval[BIAS ? 4 : 1];
+  auto load_hist = [&](int (&id)[HIST ? 8 : 1], int i0) {
+#pragma unroll
+    for (int j = 0; j < (HIST ? 8 : 1); ++j) {
+      const int i = i0 + j * kLogitThreads + tid;
+      id[j] = i < h1 ? a.h_ids[i] : -1;
+    }
+  };
+  auto load_bias = [&](int i0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * 64 + tid;
+      bid[j] = i < b1 ? a.b_ids[i] : -1;
+      bval[j] = i < b1 ? a.b_val[i] : 0.0f;
+    }
+  };
+  if constexpr (HIST)
+    if (hist) load_hist(hid, h0);
+  if constexpr (BIAS)
+    if (adds) load_bias(b0);
+  if constexpr (VEC) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = (k * kLogitThreads + tid) * N;
+      m[k] = none ? 0u : 0xffffffffu;
+      if (mask && i + N <= nv) m[k] = mask[i >> 5] >> (i & 31);
+    }
+  }
+  const uint4 zero = {0, 0, 0, 0};
+  if (hist || biased) {
+    for (int i = tid; i < kSlice / 4; i += kLogitThreads) reinterpret_cast<uint4 *>(cnt)[i] = zero;
+    __syncthreads();
+  }
+  if constexpr (HIST) {
+    const int made = h0 + max(0, min(prompt, h1 - h0));
+    for (int i0 = h0; hist && i0 < h1; i0 += 8 * kLogitThreads) {
+      if (i0 + 8 * kLogitThreads < h1) load_hist(hnext, i0 + 8 * kLogitThreads);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t v = (uint32_t)hid[j] - (uint32_t)v0;
+        if (v < (uint32_t)nv) {
+          if (i0 + j * kLogitThreads + tid >= made) atomicAdd(&cnt[v], 2u);
+          else atomicOr(&cnt[v], 1u);
+        }
+        hid[j] = hnext[j];
+      }
+    }
+  }
+  // this thread's tokens: vector k's from (k kLogitThreads + tid) N, or those
+  // from tid on, kLogitThreads apart
+  constexpr int NT = kSlice / kLogitThreads;
+  uint32_t c[HIST ? NT : 1];
+  if constexpr (HIST) {
+    if (hist) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NT; k += VEC ? 4 : 1) {
+      const int i = VEC ? (k / N * kLogitThreads + tid) * N + k % N : k * kLogitThreads + tid;
+      if constexpr (VEC) {
+        const uint4 q = hist ? *reinterpret_cast<const uint4 *>(&cnt[i]) : zero;
+        c[k] = q.x; c[k + 1] = q.y; c[k + 2] = q.z; c[k + 3] = q.w;
+        if (hist && biased) *reinterpret_cast<uint4 *>(&cnt[i]) = zero;
+      } else {
+        c[k] = hist ? cnt[i] : 0u;
+        if (hist && biased) cnt[i] = 0u;
+      }
+    }
+    if (hist && biased) __syncthreads();
+  }
+  if constexpr (BIAS) {
+    // entry after entry: LDS operations of one wave are done in their order,
+    // so equal ids add up in list order
+    for (int i0 = b0; adds && i0 < b1; i0 += 256) {
+      if (i0 > b0) load_bias(i0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t v = (uint32_t)bid[j] - (uint32_t)v0;
+        for (uint64_t in_slice = __ballot(v < (uint32_t)nv); in_slice; in_slice &= in_slice - 1) {
+          if (tid == __builtin_ctzll(in_slice)) atomicAdd(&bias[v], bval[j]);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+      }
+    }
+  }
+  if (biased) __syncthreads();
+  auto count_of = [&](int k) { return HIST ? c[k] : 0u; };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = (k * kLogitThreads + tid) * N;
+      if (i + N > nv) {  // the row's end, inside a vector
+        for (int j = 0; j < N && i + j < nv; ++j) {
+          uint32_t q = 0;
+#pragma unroll
+          for (int e = 0; e < N; ++e) q = e == j ? count_of(k * N + e) : q;
+          const float b = biased ? bias[i + j] : 0.0f;
+          T x = in[i + j];
+          if (q || b != 0.0f) x = from_f<T>(adjusted(to_f<T>(x), q, b, w));
+          const bool allowed = !none && (!mask || (mask[(i + j) >> 5] >> ((i + j) & 31) & 1));
+          out[i + j] = allowed ? x : from_f<T>(-INFINITY);
+        }
+        continue;
+      }
+      uint32_t seen = 0;
+      float b[N] = {};
+      bool off = false;  // any bias
+#pragma unroll
+      for (int j = 0; j < N; ++j) seen |= count_of(k * N + j);
+#pragma unroll
+      for (int j = 0; j < N; j += 4) {
+        if (biased) {
+          const f32x4 q = *reinterpret_cast<const f32x4 *>(&bias[i + j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            b[j + e] = q[e];
+            off |= q[e] != 0.0f;
+          }
+        }
+      }
+      const bool masked = ~m[k] & ((1u << N) - 1);
+      if (!seen && !off && !masked) {  // these logits stay as they are
+        if (!inplace) st16(out + i, u[k]);
+        continue;
+      }
+      if (inplace) u[k] = ld16(in + i);
+      T x[N];
+      __builtin_memcpy(x, &u[k], 16);
+      if (seen || off) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          x[j] = from_f<T>(adjusted(to_f<T>(x[j]), count_of(k * N + j), b[j], w));
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (!(m[k] >> j & 1)) x[j] = from_f<T>(-INFINITY);
+      __builtin_memcpy(&u[k], x, 16);
+      st16(out + i, u[k]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      const int i = k * kLogitThreads + tid;
+      if (i >= nv) break;
+      const bool allowed = !none && (!mask || (mask[i >> 5] >> (i & 31) & 1));
+      const float b = biased ? bias[i] : 0.0f;
+      T x = in[i];
+      if (count_of(k) || b != 0.0f) x = from_f<T>(adjusted(to_f<T>(x), count_of(k), b, w));
+      out[i] = allowed ? x : from_f<T>(-INFINITY);
+    }
+  }
+}
+
+template <typename T, bool HIST, bool BIAS> static void run_vec(const LogitsArgs &a, dim3 grid, hipStream_t st) {
+  const int64_t es = sizeof(T);
+  const bool vec = ((uintptr_t)a.in | (uintptr_t)a.out) % 16 == 0 && a.in_ld * es % 16 == 0 && a.out_ld * es % 16 == 0;
+  if (vec) hipLaunchKernelGGL((logits_adjust_kernel<T, HIST, BIAS, true>), grid, dim3(kLogitThreads), 0, st, a);
+  else hipLaunchKernelGGL((logits_adjust_kernel<T, HIST, BIAS, false>), grid, dim3(kLogitThreads), 0, st, a);
+}
+template <typename T> static void run_rules(const LogitsArgs &a, dim3 grid, hipStream_t st) {
+  const bool hist = a.h_off && a.n_hist > 0, bias = a.b_off && a.n_bias > 0;
+  if (hist && bias) run_vec<T, true, true>(a, grid, st);
+  else if (hist) run_vec<T, true, false>(a, grid, st);
+  else if (bias) run_vec<T, false, true>(a, grid, st);
+  else run_vec<T, false, false>(a, grid, st);
 }
 
 hipError_t launch_logits_adjust(const LogitsArgs &a, hipStream_t st) {
@@ -113,9 +261,9 @@ hipError_t launch_logits_adjust(const LogitsArgs &a, hipStream_t st) {
       b.n_masks -= r0;
     }
     const dim3 grid((unsigned)((a.V + kSlice - 1) / kSlice), (unsigned)b.R);
-    if (a.type == 0) hipLaunchKernelGGL(logits_adjust_kernel<float>, grid, dim3(kLogitThreads), 0, st, b);
-    else if (a.type == 1) hipLaunchKernelGGL(logits_adjust_kernel<f16>, grid, dim3(kLogitThreads), 0, st, b);
-    else hipLaunchKernelGGL(logits_adjust_kernel<bf16>, grid, dim3(kLogitThreads), 0, st, b);
+    if (a.type == 0) run_rules<float>(b, grid, st);
+    else if (a.type == 1) run_rules<f16>(b, grid, st);
+    else run_rules<bf16>(b, grid, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -77,9 +77,9 @@ Status check_logits(const jet_logits_args *a) {
   const size_t es = (size_t)type_bytes(a->type);
   if (!aligned(a->logits, es) || !aligned(a->out, es)) return bad("logits or out is not aligned");
   if (a->out == a->logits && a->out_stride != a->row_stride) return bad("in place, out_stride must be row_stride");
-  if (a->n_hist < 0 || a->n_hist > INT32_MAX) return bad("n_hist must be in 0 .. 2^31 - 1");
+  if (a->n_hist < 0 || a->n_hist > (1 << 30)) return bad("n_hist must be in 0 .. 2^30");
   if (a->hist_offsets && a->n_hist > 0 && !a->hist_ids) return bad("hist_ids is NULL");
-  if (a->n_bias < 0 || a->n_bias > INT32_MAX) return bad("n_bias must be in 0 .. 2^31 - 1");
+  if (a->n_bias < 0 || a->n_bias > (1 << 30)) return bad("n_bias must be in 0 .. 2^30");
   if (a->bias_offsets && a->n_bias > 0 && (!a->bias_ids || !a->bias_values)) return bad("bias_ids or bias_values is NULL");
   if (a->n_masks < 0) return bad("n_masks must be >= 0");
   if (a->masks) {

@@ -137,7 +137,7 @@ def logits(**over):
 @pytest.mark.parametrize("over", [
     dict(n_rows=-1), dict(n_rows=(1 << 20) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(type=3),
     dict(logits=None), dict(out=None), dict(logits=A + 2), dict(out=A + 1), dict(row_stride=99), dict(out_stride=99),
-    dict(out_stride=101), dict(n_hist=-1), dict(n_hist=1 << 31), dict(hist_ids=None), dict(n_bias=-1),
+    dict(out_stride=101), dict(n_hist=-1), dict(n_hist=(1 << 30) + 1), dict(n_bias=(1 << 30) + 1), dict(hist_ids=None), dict(n_bias=-1),
     dict(bias_ids=None), dict(bias_values=None), dict(n_masks=-1), dict(mask_stride=3), dict(masks=None),
     dict(mask_index=None, n_masks=1), dict(hist_offsets=A + 2), dict(repetition=A + 1), dict(masks=A + 2)])
 def test_bad_logits(over):
