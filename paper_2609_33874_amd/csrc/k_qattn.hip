@@ -1,19 +1,8 @@
 // Attention over a cache held in 8 bits (jet.h: jet_qcache_attention).
-//
-// For row i of a sequence and query head h over KV head h / G:
-//   s_j = scale 2^(ek_j) sum_d q_d k_jd,  o = sum_j softmax(s)_j 2^(ev_j) v_j
-// over the tokens j that the row sees, in one pass with the running maximum and
-// sum of the softmax. The 8-bit values are exact in f16, so both products run
-// on the matrix cores in f16 with the scales outside of them: K's on the
-// scores, V's on the probabilities. A probability goes into the second product
-// as p 2^(ev - M) 2^15 in f16, M the largest V exponent met so far (the
-// accumulators are in units of 2^(M - 15) and rescaled when M grows), so that
-// what it loses is its rounding to 11 bits, or 2^-40 of the largest value.
-// bf16 queries enter as f16 times a power of two that puts a row's largest
-// value in [2^14, 2^15): exact down to 2^-30 of it.
+// Few query slots: see qattn.h for the arithmetic, k_qattn_rows.hip for many.
 #include <algorithm>
 
-#include "qcache.h"
+#include "qattn.h"
 
 namespace jetk {
 
@@ -46,16 +35,6 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
       w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
     }
   }
-}
-
-// Partial results of a split: o [split][row * Hq + head][hd] (not divided by
-// l), then m and l [split][row * Hq + head].
-struct Parts {
-  float *o, *m, *l;
-};
-__device__ __host__ __forceinline__ Parts parts_of(void *ws, int64_t n, int nsplit, int hd) {
-  float *o = (float *)ws;
-  return {o, o + n * nsplit * hd, o + n * nsplit * (hd + 1)};
 }
 
 // One workgroup per (block of 16 QB query slots and split of the keys, KV
@@ -101,40 +80,8 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
       const int pos = sq.pos0 + i;
       vis[qb] = pos < 0 ? 0 : a.causal ? pos + 1 : sq.len;
       vis_min = min(vis_min, vis[qb]);
-      const T *q = (const T *)a.q.p + (int64_t)(sq.row0 + i) * a.q.rs + (int64_t)head * a.q.hs + g * (HD / 4);
-      float x[NK][8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int ks = 0; ks < NK; ++ks) {
-        if (a.q.vec) {
-          const uint4 u = ld16(q + ks * 8);
-          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[ks][2 * j] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] & 0xffff)));
-            x[ks][2 * j + 1] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] >> 16)));
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[ks][j] = to_f<T>(q[ks * 8 + j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[ks][j]) & 0x7fffffffu);
-      }
-      float up = 1.0f;
-      fq[qb] = a.scale * kLog2e;
-      if constexpr (sizeof(T) == 2 && !__is_same(T, f16)) {
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        // largest value 2^x f, f in [1, 2): times 2^(14 - x), and back on the scores
-        const int e = min(max((int)(top >> 23) - 127, -112), 127);
-        if (top) up = pow2i(14 - e);
-        if (top) fq[qb] *= pow2i(e - 14);
-      }
-#pragma unroll
-      for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) qf[qb][ks].v[j] = (f16)(x[ks][j] * up);
+      const T *q = (const T *)a.q.p + (int64_t)(sq.row0 + i) * a.q.rs + (int64_t)head * a.q.hs;
+      fq[qb] = load_query<T, NK>(qf[qb], q, g * (HD / 4), 8, a.q.vec, a.scale * kLog2e);
     }
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) vis_min = min(vis_min, __shfl_xor(vis_min, o));
@@ -187,13 +134,9 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
       }
       const int ke0 = __builtin_amdgcn_readfirstlane(cur.ke[0]), ke1 = __builtin_amdgcn_readfirstlane(cur.ke[1]);
       const int ve0 = __builtin_amdgcn_readfirstlane(cur.ve[0]), ve1 = __builtin_amdgcn_readfirstlane(cur.ve[1]);
-      const float nan = __uint_as_float(0x7fc00000u);
-      const float ks2[2] = {ke0 == kExpNaN ? nan : pow2i(ke0 - kExpBias), ke1 == kExpNaN ? nan : pow2i(ke1 - kExpBias)};
-      const int Mn = max(M, max(ve0 == kExpNaN ? 0 : ve0, ve1 == kExpNaN ? 0 : ve1));
-      // the tile's V scales in units of 2^(Mn - 15), and the accumulators' old unit in the new one's
-      const float vs[2] = {ve0 == kExpNaN ? nan : ve0 - Mn < -126 ? 0.0f : pow2i(ve0 - Mn + 15),
-                           ve1 == kExpNaN ? nan : ve1 - Mn < -126 ? 0.0f : pow2i(ve1 - Mn + 15)};
-      const float unit = M - Mn < -126 ? 0.0f : pow2i(M - Mn);
+      const float ks2[2] = {k_scale(ke0), k_scale(ke1)};
+      const int Mn = max(M, max(v_top(ve0), v_top(ve1)));
+      const float vs[2] = {v_scale(ve0, Mn), v_scale(ve1, Mn)}, unit = v_scale(M, Mn);
       M = Mn;
       const bool all_seen = k0 + kTile <= vis_min;
       Frag<f16> pf[QB];
@@ -208,17 +151,16 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
             if (!all_seen && k0 + kb * 16 + 4 * g + e >= vis[qb]) z[kb][e] = -INFINITY;
             mx = fmaxf(mx, z[kb][e]);
           }
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = query_max(mx);
         const float mn = fmaxf(m[qb], mx), ms = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m[qb] - ms);
+        const float alpha = __builtin_amdgcn_exp2f(m[qb] - ms), ms15 = ms - 15.0f;
         m[qb] = mn;
         float p[2][4], sum = 0.0f;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            p[kb][e] = __builtin_amdgcn_exp2f(z[kb][e] - ms);
+            p[kb][e] = __builtin_amdgcn_exp2f(z[kb][e] - ms15);  // 2^15 p, and l in that unit
             sum += p[kb][e];
             // (a masked key's 0 must stay 0 where the block's scale is NaN)
             p[kb][e] = z[kb][e] == -INFINITY ? 0.0f : p[kb][e] * vs[kb];
@@ -261,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
       const int q = qb * 16 + c;
       if (g == 0) {
         s_m[wave][q] = m[qb];
-        s_l[wave][q] = lt;
+        s_l[wave][q] = lt * 0x1p-15f;
       }
       // acc[i][e] is dim ND (4 g + e) + i
 #pragma unroll
@@ -349,47 +291,61 @@ __global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
   }
 }
 
-// Query slots of a sequence and KV head, and the splits of their keys: enough
-// workgroups for four on each of 256 CUs, of at least two tiles a wave.
-static int64_t slots_of(const QCache &c, const QBatch &b, int Hq) { return (int64_t)std::max(b.max_rows, 1) * (Hq / c.H); }
-static int splits_of(const QCache &c, const QBatch &b, int Hq) {
-  const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots_of(c, b, Hq) + 15) / 16);
-  const int64_t most = std::min<int64_t>((std::max<int64_t>(b.max_len, 1) + 255) / 256, kMaxSplit);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (1024 + units - 1) / units));
+// The kernel and the splits of a launch: query slots of a sequence and KV head
+// (rows * heads of its group) up to kFewSlots take the kernel above, more take
+// the one of k_qattn_rows.hip. Splits: enough workgroups to fill 256 CUs (four
+// each, or two of the larger ones), of at least 256 or 512 keys.
+constexpr int64_t kFewSlots = 32;
+struct Plan {
+  bool few;
+  int nsplit;
+};
+static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
+  const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::max<int64_t>(b.max_len, 1);
+  const bool few = slots <= kFewSlots;
+  const int64_t block = few ? 16 : qattn_rows_block(c.hd), fill = few ? 1024 : 512, least = few ? 256 : 512;
+  const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
+  const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
+  return {few, (int)std::max<int64_t>(1, std::min<int64_t>(most, (fill + units - 1) / units))};
 }
 
 int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
-  const int n = splits_of(c, b, Hq);
+  const int n = plan_of(c, b, Hq).nsplit;
   return n == 1 ? 0 : (int64_t)b.n_rows * Hq * n * (c.hd + 2) * 4;
 }
 
-template <typename T, typename O, int FMT, int HD>
-static hipError_t run_split(const QAttn &a, hipStream_t st) {
-  const int nsplit = splits_of(a.c, a.b, a.Hq);
-  const int64_t blocks = std::min<int64_t>((slots_of(a.c, a.b, a.Hq) + 15) / 16, 65536);
-  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)(blocks * nsplit), a.c.H, a.b.n_seq),
-                     dim3(64 * kWaves), 0, st, a, nsplit);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || nsplit == 1) return e;
+template <typename O, int HD> static hipError_t run_join(const QAttn &a, int nsplit, hipStream_t st) {
   const unsigned rows = (unsigned)std::min(std::max(a.b.max_rows, 1), 65536);
   hipLaunchKernelGGL((qattn_join_kernel<O, HD>), dim3(rows, a.Hq, a.b.n_seq), dim3(256), 0, st, a, nsplit);
   return hipGetLastError();
 }
 
-template <typename T, typename O, int FMT>
-static hipError_t run_hd(const QAttn &a, hipStream_t st) {
-  if (a.c.hd == 64) return run_split<T, O, FMT, 64>(a, st);
-  if (a.c.hd == 128) return run_split<T, O, FMT, 128>(a, st);
-  return run_split<T, O, FMT, 256>(a, st);
+template <typename T, typename O, int FMT, int HD>
+static hipError_t run_few(const QAttn &a, int nsplit, hipStream_t st) {
+  const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H);
+  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)((slots + 15) / 16 * nsplit), a.c.H, a.b.n_seq),
+                     dim3(64 * kWaves), 0, st, a, nsplit);
+  return hipGetLastError();
 }
-template <typename T, typename O> static hipError_t run_fmt(const QAttn &a, hipStream_t st) {
-  return a.c.fmt == 0 ? run_hd<T, O, 0>(a, st) : run_hd<T, O, 1>(a, st);
+
+template <typename T, typename O, int FMT, int HD> static hipError_t run_hd(const QAttn &a, hipStream_t st) {
+  const Plan p = plan_of(a.c, a.b, a.Hq);
+  const hipError_t e = p.few ? run_few<T, O, FMT, HD>(a, p.nsplit, st) : launch_qattn_rows(a, p.nsplit, st);
+  return e != hipSuccess || p.nsplit == 1 ? e : run_join<O, HD>(a, p.nsplit, st);
+}
+template <typename T, typename O, int FMT> static hipError_t run_fmt(const QAttn &a, hipStream_t st) {
+  if (a.c.hd == 64) return run_hd<T, O, FMT, 64>(a, st);
+  if (a.c.hd == 128) return run_hd<T, O, FMT, 128>(a, st);
+  return run_hd<T, O, FMT, 256>(a, st);
+}
+template <typename T, typename O> static hipError_t run_types(const QAttn &a, hipStream_t st) {
+  return a.c.fmt == 0 ? run_fmt<T, O, 0>(a, st) : run_fmt<T, O, 1>(a, st);
 }
 
 hipError_t launch_qattn(const QAttn &a, hipStream_t st) {
   if (a.b.n_seq <= 0 || a.b.n_rows <= 0) return hipSuccess;
-  if (a.q.type == 1) return a.out.type == 0 ? run_fmt<f16, float>(a, st) : run_fmt<f16, f16>(a, st);
-  return a.out.type == 0 ? run_fmt<bf16, float>(a, st) : run_fmt<bf16, bf16>(a, st);
+  if (a.q.type == 1) return a.out.type == 0 ? run_types<f16, float>(a, st) : run_types<f16, f16>(a, st);
+  return a.out.type == 0 ? run_types<bf16, float>(a, st) : run_types<bf16, bf16>(a, st);
 }
 
 }  // namespace jetk

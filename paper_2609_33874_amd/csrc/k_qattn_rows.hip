@@ -1,0 +1,472 @@
+// Attention over a cache held in 8 bits, many query slots: see qattn.h for the
+// arithmetic. A workgroup of four waves takes 64 QB query slots of one
+// (sequence, KV head); tiles of 64 keys are turned into f16 once for all of
+// them on their way into LDS (two stages: while one is computed the next one
+// is converted and the one after it loaded into registers), so that per key
+// tile and wave the conversion is a quarter of what it would be in the waves'
+// own registers, where it costs more than the products.
+// What bounds it: the vector instructions of the softmax (about six and an
+// exponential per score) and the LDS reads of K and V, each about as long as
+// the matrix instructions.
+// With own rows (candidate scoring) the keys of a query's own candidate follow
+// as 16-bit tiles of the same stream; there no split is made and every query
+// runs the same operations in the same order whatever block it lies in.
+#include <algorithm>
+
+#include "gemm_core.h"
+#include "qattn.h"
+
+namespace jetk {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Work of a launch: units (sequence, KV head) of `per` workgroups each. The
+// workgroups of a unit run on one XCD (they share its keys in that L2), which
+// deals workgroup w to XCD w % 8.
+struct Work {
+  int64_t unit;
+  int part;
+};
+__device__ __forceinline__ Work work_of(int64_t w, int64_t units, int per) {
+  const int64_t even = units / 8 * 8 * per;
+  if (w >= even) return {units / 8 * 8 + (w - even) / per, (int)((w - even) % per)};
+  return {w / 8 / per * 8 + w % 8, (int)(w / 8 % per)};
+}
+
+// A thread's index that the compiler takes for a new value at each place: what
+// is computed from it stays inside the loop (moved out of it, the addresses of
+// a whole tile took registers that the accumulators need).
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
+__global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAttn a, OwnRows own, int blocks,
+                                                                           int nsplit) {
+  constexpr int NW = 4, KT = 64, BLOCK = 16 * QB * NW, NK = HD / 32, ND = HD / 16;
+  constexpr int RB = HD * 2, CPR = HD / 8;                // bytes and 16-byte chunks of an f16 row
+  constexpr int PLANE = KT * RB, STAGE = 2 * PLANE;       // K, then V
+  constexpr int RC = HD / 16, LD = KT * RC / (64 * NW);   // 16-byte chunks of an 8-bit row, and a thread's of a tile
+  extern __shared__ __align__(16) char smem[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.Hq / a.c.H, lb = a.c.lb;
+  const int64_t units = OWN ? own.n_items : (int64_t)a.b.n_seq * a.c.H;
+  const int per = OWN ? 1 : blocks * nsplit;
+
+  // chunk c of row r lies at c ^ kswz(r) (K: the 16 rows of a fragment read) or
+  // c ^ vswz(r) (V: the rows of a transposed read)
+  auto kswz = [](int r) { return r & (CPR < 16 ? CPR - 1 : 15); };
+  auto vswz = [](int r) { return (r & (CPR < 16 ? 3 : 7)) << 1; };
+
+  for (int64_t w = blockIdx.x; w < units * per; w += gridDim.x) {
+    // this workgroup's sequence, KV head, rows and keys
+    int h, sp = 0, sb0 = 0, row0, rows, pos0, len;
+    int64_t slot0;
+    int it_slots = 0, npre_item = 0;
+    AttnItem it{};
+    if constexpr (OWN) {
+      it = own.items[w];
+      h = it.kvh;
+      row0 = own.qs.qrow0[it.q];
+      rows = own.qs.nrows[it.q];
+      slot0 = own.qs.pre_slot0[it.q];
+      len = own.qs.pre_len[it.q];
+      pos0 = len;  // (every row sees the whole prefix)
+      sb0 = it.slot0;
+      it_slots = it.slot0 + it.nslots;
+    } else {
+      const Work x = work_of(w, units, per);
+      h = (int)(x.unit % a.c.H);
+      sp = x.part % nsplit;
+      sb0 = x.part / nsplit * BLOCK;
+      const QSeq sq = qseq(a.b, a.c, (int)(x.unit / a.c.H));
+      row0 = sq.row0;
+      rows = sq.n;
+      slot0 = sq.slot0;
+      len = sq.len;
+      pos0 = sq.pos0;
+    }
+    const int64_t base = ((int64_t)h * a.c.S + slot0) * HD, ebase = (int64_t)h * (a.c.S >> lb) + (slot0 >> lb);
+    const uint8_t *K = a.c.k + base, *V = a.c.v + base, *KE = a.c.ke + ebase, *VE = a.c.ve + ebase;
+    const int slots = OWN ? it_slots : rows * G;
+
+    for (int sb = sb0; sb < slots; sb += OWN ? slots : blocks * BLOCK) {
+      const int tid = here(threadIdx.x), lane = tid & 63, g = lane >> 4, l16 = lane & 15;
+      const int r_last = (min(sb + BLOCK, slots) - 1) / G;  // last row of the block, in the sequence
+      const int kend = OWN || !a.causal ? len : max(0, pos0 + r_last + 1);
+      const int ntile = (kend + KT - 1) / KT, tps = (ntile + nsplit - 1) / nsplit;
+      const int key0 = sp * tps * KT, key1 = min(kend, (sp + 1) * tps * KT);
+
+      // The stream of key tiles: the cache's (cs < 0), then for every candidate
+      // with rows in the block (first body row cs) its rows up to the block's
+      // last one, in tiles that start at cs. nk = 0 past the end.
+      struct Tile {
+        int cs, t0, nk;
+      };
+      const int r_first = row0 + sb / G, r_end = row0 + r_last;
+      int cs_first = 0, n_a = 1, n_b = 1;
+      if constexpr (OWN) {
+        cs_first = r_first - own.row_t[r_first] + 1;
+        n_a = own.row_n[min(r_first + lane, r_end)];
+        n_b = own.row_n[min(r_first + 64 + lane, r_end)];
+      }
+      auto own_n = [&](int cs) {  // body rows of the candidate that starts at row cs
+        const int i = max(cs, r_first) - r_first;
+        return i >= 64 ? __builtin_amdgcn_readlane(n_b, i - 64) : __builtin_amdgcn_readlane(n_a, i);
+      };
+      auto own_tile = [&](int cs, int ts) {
+        if (cs > r_end) return Tile{0, 0, 0};
+        return Tile{cs, ts, min(KT, min(cs + own_n(cs) - 1, r_end) - ts + 1)};
+      };
+      auto next_tile = [&](const Tile &t) {
+        if (t.nk == 0) return t;
+        if (!OWN || t.cs < 0) {
+          const int kb = t.t0 + KT;
+          if (kb < key1) return Tile{-1, kb, min(KT, key1 - kb)};
+          if constexpr (OWN) return own_tile(cs_first, cs_first);
+          return Tile{0, 0, 0};
+        }
+        const int n = own_n(t.cs);
+        if (t.t0 + KT <= min(t.cs + n - 1, r_end)) return own_tile(t.cs, t.t0 + KT);
+        return own_tile(t.cs + n, t.cs + n);
+      };
+
+      // 8-bit rows of a tile into registers (rows past its end: its last one),
+      // and the tile's scale bytes: lane l (mod 8) the one of K (l < 4) or V of
+      // keys 16 (l mod 4) ..
+      uint4 rk[LD], rv[LD];
+      int re = 0;
+      auto load = [&](const Tile &t) {
+        const int tid = here(threadIdx.x), lane = tid & 63;
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+          const int x = i * 256 + tid;
+          const int64_t at = (int64_t)(t.t0 + min(x / RC, t.nk - 1)) * HD + x % RC * 16;
+          rk[i] = ld16(K + at);
+          rv[i] = ld16(V + at);
+        }
+        const int b = (t.t0 + min((lane & 3) * 16, t.nk - 1)) >> lb;
+        re = (lane & 4 ? VE : KE)[b];
+      };
+      // ... and from there into a stage
+      auto store = [&](int stage) {
+        char *dst = smem + stage * STAGE;
+        const int tid = here(threadIdx.x);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+          const int x = i * 256 + tid, r = x / RC, c = x % RC * 2;
+          auto put = [&](char *row, int ca, int cb, const uint4 &u) {
+            const uint2 p = f16x4_of<FMT>(u.x), q = f16x4_of<FMT>(u.y), s = f16x4_of<FMT>(u.z), t = f16x4_of<FMT>(u.w);
+            st16(row + ca * 16, make_uint4(p.x, p.y, q.x, q.y));
+            st16(row + cb * 16, make_uint4(s.x, s.y, t.x, t.y));
+          };
+          put(dst + r * RB, c ^ kswz(r), (c + 1) ^ kswz(r), rk[i]);
+          put(dst + PLANE + r * RB, c ^ vswz(r), (c + 1) ^ vswz(r), rv[i]);
+        }
+      };
+      // 16-bit rows of an own tile straight into a stage
+      auto load_own = [&](const Tile &t, int stage) {
+        constexpr int RPL = 64 / CPR;  // rows of a wave's load
+        char *dst = smem + stage * STAGE;
+        const f16 *Ko = own.K + (int64_t)h * own.s_suf * HD, *Vo = own.V + (int64_t)h * own.s_suf * HD;
+#pragma unroll
+        for (int i = 0; i < KT / RPL / NW; ++i) {
+          const int blk = i * NW + wave, r = blk * RPL + lane / CPR, c = lane % CPR;
+          const int64_t off = (int64_t)(t.t0 + min(r, t.nk - 1)) * HD;
+          __builtin_amdgcn_global_load_lds((const void *)(Ko + off + (c ^ kswz(r)) * 8), (lds_void *)(dst + blk * 1024),
+                                           16, 0, 0);
+          __builtin_amdgcn_global_load_lds((const void *)(Vo + off + (c ^ vswz(r)) * 8),
+                                           (lds_void *)(dst + PLANE + blk * 1024), 16, 0, 0);
+        }
+      };
+
+      Tile cur = key0 < key1 ? Tile{-1, key0, min(KT, key1 - key0)} : Tile{0, 0, 0};
+      if (OWN && cur.nk == 0) cur = own_tile(cs_first, cs_first);
+      if (cur.nk > 0 && cur.cs < 0) load(cur);
+
+      int row[QB], vis[QB], first[QB], vis_min = kend;
+      Frag<f16> qf[QB][NK];
+      float fq[QB], m[QB], l[QB];
+      f32x4 acc[QB][ND];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const int s = sb + (wave * QB + qb) * 16 + l16;
+        const int i = (s < slots ? s : sb) / G, head = h * G + (s < slots ? s : sb) % G, pos = pos0 + i;
+        row[qb] = row0 + i;
+        vis[qb] = OWN ? len : pos < 0 ? 0 : a.causal ? pos + 1 : len;
+        vis_min = min(vis_min, vis[qb]);
+        first[qb] = OWN && s < slots ? row[qb] - own.row_t[row[qb]] + 1 : -1;
+        const T *q = (const T *)a.q.p + (int64_t)row[qb] * a.q.rs + (int64_t)head * a.q.hs;
+        fq[qb] = load_query<T, NK>(qf[qb], q, g * 8, 32, a.q.vec, a.scale * kLog2e);
+        m[qb] = -INFINITY;
+        l[qb] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[qb][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) vis_min = min(vis_min, __shfl_xor(vis_min, o));
+      const bool idle = sb + wave * QB * 16 >= slots;  // no query: loads and barriers only
+      int M = 0;  // V exponent byte of the accumulators' unit
+
+      int ec = re, stage = 0;  // the current tile's scale bytes
+      __syncthreads();         // the block before is done with the stages
+      if (cur.nk > 0) {
+        if (cur.cs < 0) store(0);
+        else load_own(cur, 0);
+      }
+      Tile ahead = next_tile(cur);
+      if (ahead.nk > 0 && ahead.cs < 0) load(ahead);
+      while (cur.nk > 0) {
+        if constexpr (OWN) wait_vmcnt<0>();  // (own tiles are loaded into LDS directly)
+        __syncthreads();                     // this tile is in place, and every wave is done with the other stage
+        const int ea = re;
+        Tile after = ahead;
+        if (ahead.nk > 0) {
+          if (ahead.cs < 0) store(stage ^ 1);
+          else load_own(ahead, stage ^ 1);
+          after = next_tile(ahead);
+          if (after.nk > 0 && after.cs < 0) load(after);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (!idle) {
+          const char *sk = smem + stage * STAGE, *sv = sk + PLANE;
+          const int lane = here(threadIdx.x) & 63, g = lane >> 4, l16 = lane & 15;
+          const bool pre = !OWN || cur.cs < 0;
+          f32x4 s[QB][4];
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          auto read_k = [&](int ks, int kb) {
+            return ld16(sk + (kb * 16 + l16) * RB + (((ks * 4 + g) ^ kswz(l16)) << 4));
+          };
+          auto score = [&](int ks, int kb, uint4 u) {
+            Frag<f16> f;
+            f.v = __builtin_bit_cast(f16x8, u);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) mma16(s[qb][kb], f, qf[qb][ks]);
+          };
+          // fragments are read one group of products ahead, and no further (the
+          // compiler would hold them all in registers)
+          if (cur.nk > 48) {
+            uint4 f[2][4];
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) f[0][kb] = read_k(0, kb);
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) {
+              if (ks + 1 < NK) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) f[(ks + 1) & 1][kb] = read_k(ks + 1, kb);
+              }
+#pragma unroll
+              for (int kb = 0; kb < 4; ++kb) score(ks, kb, f[ks & 1][kb]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          } else {
+#pragma unroll
+            for (int kb = 0; kb < 3; ++kb)
+              if (kb * 16 < cur.nk) {
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) score(ks, kb, read_k(ks, kb));
+              }
+          }
+          int ve[4], Mn = M;
+          float ks2[4];
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) {
+            // (own rows are as they are: scale 1)
+            ks2[kb] = pre ? k_scale(__builtin_amdgcn_readlane(ec, kb)) : 1.0f;
+            ve[kb] = pre ? __builtin_amdgcn_readlane(ec, 4 + kb) : kExpBias;
+            Mn = max(Mn, v_top(ve[kb]));
+          }
+          const float unit = v_scale(M, Mn);
+          const bool same = ve[0] == Mn && ve[1] == Mn && ve[2] == Mn && ve[3] == Mn;
+          M = Mn;
+          Frag<f16> pf[QB][2];
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            float mx = -INFINITY;
+            if (pre && cur.t0 + KT <= min(vis_min, key1)) {
+#pragma unroll
+              for (int kb = 0; kb < 4; ++kb) {
+                const float f = ks2[kb] * fq[qb];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  s[qb][kb][e] *= f;
+                  mx = fmaxf(mx, s[qb][kb][e]);
+                }
+              }
+            } else {
+              // last key of the tile that the query sees: the prefix's, or the
+              // query's own row of its candidate's tile
+              const int last = pre ? min(cur.nk, vis[qb] - cur.t0) - 1
+                                   : (first[qb] == cur.cs ? min(cur.nk - 1, row[qb] - cur.t0) : -1);
+#pragma unroll
+              for (int kb = 0; kb < 4; ++kb) {
+                const float f = ks2[kb] * fq[qb];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float z = kb * 16 + 4 * g + e <= last ? s[qb][kb][e] * f : -INFINITY;
+                  s[qb][kb][e] = z;
+                  mx = fmaxf(mx, z);
+                }
+              }
+            }
+            mx = query_max(mx);
+            const float mn = fmaxf(m[qb], mx), ms = mn == -INFINITY ? 0.0f : mn, ms15 = ms - 15.0f;
+            const float al = __builtin_amdgcn_exp2f(m[qb] - ms);
+            m[qb] = mn;
+            float p[4][4], sum = 0.0f;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                p[kb][e] = __builtin_amdgcn_exp2f(s[qb][kb][e] - ms15);  // 2^15 p, and l in that unit
+                sum += p[kb][e];
+              }
+            l[qb] = l[qb] * al + sum;
+            if (!same) {
+#pragma unroll
+              for (int kb = 0; kb < 4; ++kb) {
+                const float f = v_scale(ve[kb], Mn);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)  // (a masked key's 0 must stay 0 where the scale is NaN)
+                  p[kb][e] = s[qb][kb][e] == -INFINITY ? 0.0f : p[kb][e] * f;
+              }
+            }
+            const float au = al * unit;
+            if (__any(au != 1.0f)) {
+#pragma unroll
+              for (int d = 0; d < ND; ++d) acc[qb][d] *= au;
+            }
+#pragma unroll
+            for (int mm = 0; mm < 2; ++mm) {
+              const uint4 u = make_uint4(f2h2(p[2 * mm][0], p[2 * mm][1]), f2h2(p[2 * mm][2], p[2 * mm][3]),
+                                         f2h2(p[2 * mm + 1][0], p[2 * mm + 1][1]), f2h2(p[2 * mm + 1][2], p[2 * mm + 1][3]));
+              pf[qb][mm].v = __builtin_bit_cast(f16x8, u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          // V transposed on the way out of LDS: lane l supplies 4 elements of
+          // key 4 g + (l % 16) / 4 and receives keys 4 g .. + 3 of dim l % 16
+#pragma unroll
+          for (int mm = 0; mm < 2; ++mm) {
+            if (mm * 32 >= cur.nk) continue;
+            const int vr = 4 * g + (l16 >> 2);  // (16 and 32 rows on have the same swizzle)
+            const char *at = sv + (mm * 32 + vr) * RB + (l16 & 1) * 8;
+            auto read_v = [&](int d, int half) {
+              const char *p = at + (((2 * d + (l16 >> 1 & 1)) ^ vswz(vr)) << 4) + half * 16 * RB;
+              typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+              return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_void *)p);
+            };
+            constexpr int DB = 4;
+            s16x4 f[2][DB][2];
+#pragma unroll
+            for (int d = 0; d < DB; ++d) f[0][d][0] = read_v(d, 0), f[0][d][1] = read_v(d, 1);
+#pragma unroll
+            for (int d0 = 0; d0 < ND; d0 += DB) {
+              if (d0 + DB < ND) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                  f[(d0 / DB + 1) & 1][d][0] = read_v(d0 + DB + d, 0);
+                  f[(d0 / DB + 1) & 1][d][1] = read_v(d0 + DB + d, 1);
+                }
+              }
+#pragma unroll
+              for (int d = 0; d < DB; ++d) {
+                Frag<f16> v;
+                v.v = __builtin_bit_cast(f16x8, __builtin_shufflevector(f[d0 / DB & 1][d][0], f[d0 / DB & 1][d][1], 0, 1,
+                                                                        2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) mma16(acc[qb][d0 + d], v, pf[qb][mm]);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        }
+        ec = ea;
+        cur = ahead;
+        ahead = after;
+        stage ^= 1;
+      }
+
+      {
+      const int lane = here(threadIdx.x) & 63, g = lane >> 4, l16 = lane & 15;
+      const float up = pow2i(max(M - kExpBias - 15, -126));
+      const int64_t n = (int64_t)a.b.n_rows * a.Hq;
+      const Parts parts = parts_of(a.ws, n, nsplit, HD);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float lt = l[qb] + __shfl_xor(l[qb], 16);
+        lt += __shfl_xor(lt, 32);
+        lt *= 0x1p-15f;
+        const int s = sb + (wave * QB + qb) * 16 + l16, head = h * G + s % G;
+        if (s >= slots) continue;
+        const int64_t row = row0 + s / G, at = row * a.Hq + head;
+        if (!OWN && nsplit > 1) {
+          float *o = parts.o + (sp * n + at) * HD + 4 * g;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4 *>(o + 16 * d) = acc[qb][d] * up;
+          if (g == 0) {
+            parts.m[sp * n + at] = m[qb];
+            parts.l[sp * n + at] = lt;
+          }
+          continue;
+        }
+        const float inv = lt == 0.0f ? 0.0f : up / lt;
+        O *o = (O *)a.out.p + row * a.out.rs + (int64_t)head * a.out.hs + 4 * g;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const f32x4 x = acc[qb][d] * inv;
+          if (a.out.vec) {
+            if constexpr (sizeof(O) == 2)
+              *reinterpret_cast<uint2 *>(o + 16 * d) = make_uint2(pack2<O>(x[0], x[1]), pack2<O>(x[2], x[3]));
+            else *reinterpret_cast<f32x4 *>(o + 16 * d) = x;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[16 * d + e] = from_f<O>(x[e]);
+          }
+        }
+        if (a.lse && g == 0) a.lse[at] = lt == 0.0f ? -INFINITY : m[qb] * kLn2 + logf(lt);
+      }
+      }
+    }
+  }
+}
+
+// Query slots of a workgroup: 128, or 64 of head_dim 256 (registers).
+int qattn_rows_block(int hd) { return hd == 256 ? 64 : 128; }
+
+template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
+static hipError_t run_rows(const QAttn &a, const OwnRows &own, int nsplit, hipStream_t st) {
+  constexpr int lds = 2 * 2 * 64 * HD * 2, BLOCK = 64 * QB;
+  const auto kernel = qattn_rows_kernel<T, O, FMT, HD, QB, OWN>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H);
+  const int blocks = (int)std::min<int64_t>((slots + BLOCK - 1) / BLOCK, 1 << 20);
+  const int64_t total = OWN ? own.n_items : (int64_t)a.b.n_seq * a.c.H * blocks * nsplit;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(total, 1 << 20)), dim3(256), lds, st, a, own, blocks,
+                     nsplit);
+  return hipGetLastError();
+}
+
+template <typename T, typename O, int FMT>
+static hipError_t rows_hd(const QAttn &a, int nsplit, hipStream_t st) {
+  if (a.c.hd == 64) return run_rows<T, O, FMT, 64, 2, false>(a, {}, nsplit, st);
+  if (a.c.hd == 128) return run_rows<T, O, FMT, 128, 2, false>(a, {}, nsplit, st);
+  return run_rows<T, O, FMT, 256, 1, false>(a, {}, nsplit, st);
+}
+template <typename T, typename O> static hipError_t rows_fmt(const QAttn &a, int nsplit, hipStream_t st) {
+  return a.c.fmt == 0 ? rows_hd<T, O, 0>(a, nsplit, st) : rows_hd<T, O, 1>(a, nsplit, st);
+}
+
+hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st) {
+  if (a.q.type == 1) return a.out.type == 0 ? rows_fmt<f16, float>(a, nsplit, st) : rows_fmt<f16, f16>(a, nsplit, st);
+  return a.out.type == 0 ? rows_fmt<bf16, float>(a, nsplit, st) : rows_fmt<bf16, bf16>(a, nsplit, st);
+}
+
+}  // namespace jetk

@@ -109,6 +109,8 @@ Status attention(const jet_qcache *c, const jet_qcache_batch *b, int32_t n_q_hea
   if (causal != 0 && causal != 1) return Status::err(JET_E_INVALID, "causal must be 0 or 1");
   TRY(check_rows(q, "q", 1 << JET_T_F16 | 1 << JET_T_BF16, b->n_rows));
   TRY(check_out_rows(out, "out", 1 << JET_T_F32 | 1 << q->type, b->n_rows, n_q_heads));
+  if ((int64_t)b->n_rows * (n_q_heads / c->n_heads) > (1 << 30))
+    return Status::err(JET_E_INVALID, "n_rows times the query heads of a KV head exceeds 2^30");
   if ((uintptr_t)lse % 4) return Status::err(JET_E_INVALID, "lse is not aligned");
   const jetk::QCache qc = cache_of(*c);
   const jetk::QBatch qb = batch_of(*b);
