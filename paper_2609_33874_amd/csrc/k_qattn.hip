@@ -251,50 +251,67 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
   }
 }
 
-// One workgroup per (row of a sequence, query head): the splits' results
-// joined. Rows of no sequence have no results and are left out.
-template <typename O, int HD>
+// The splits' results of a (row of a sequence, query head) joined, by W waves:
+// every W-th split each, then added up in LDS. A workgroup takes 4 / W heads.
+// Rows of no sequence have no results and are left out.
+template <typename O, int HD, int W>
 __global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
-  constexpr int D = HD / 64;
-  __shared__ float s_m[4], s_l[4], s_o[4][HD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.y;
+  constexpr int D = HD / 64, N = 4 / W;
+  __shared__ float s_l[4], s_o[4][HD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave % W;
+  const int head = blockIdx.y * N + wave / W;
   const QSeq sq = qseq(a.b, a.c, blockIdx.z);
   const int64_t n = (int64_t)a.b.n_rows * a.Hq;
   const Parts parts = parts_of(a.ws, n, nsplit, HD);
   for (int i = blockIdx.x; i < sq.n; i += gridDim.x) {
     const int64_t row = sq.row0 + i, at = row * a.Hq + head;
-    // every wave finds the maximum over all splits, then adds up every fourth one
-    float mm = -INFINITY;
-    for (int s = lane; s < nsplit; s += 64) mm = fmaxf(mm, parts.m[s * n + at]);
-    mm = warp_max(mm);
-    const float ms = mm == -INFINITY ? 0.0f : mm;
-    float l = 0.0f, o[D] = {};
+    float mm = -INFINITY, l = 0.0f, o[D] = {};
+    if (head < a.Hq) {
+      // every wave finds the maximum over all splits
+      for (int s = lane; s < nsplit; s += 64) mm = fmaxf(mm, parts.m[s * n + at]);
+      mm = warp_max(mm);
+      const float ms = mm == -INFINITY ? 0.0f : mm;
 #pragma unroll 8
-    for (int s = wave; s < nsplit; s += 4) {
-      const float f = __builtin_amdgcn_exp2f(parts.m[s * n + at] - ms);
-      l += parts.l[s * n + at] * f;
-      const float *p = parts.o + (s * n + at) * HD + lane * D;
+      for (int s = sub; s < nsplit; s += W) {
+        const float f = __builtin_amdgcn_exp2f(parts.m[s * n + at] - ms);
+        l += parts.l[s * n + at] * f;
+        const float *p = parts.o + (s * n + at) * HD + lane * D;
 #pragma unroll
-      for (int d = 0; d < D; ++d) o[d] += p[d] * f;
+        for (int d = 0; d < D; ++d) o[d] += p[d] * f;
+      }
     }
-    __syncthreads();
-    if (lane == 0) s_l[wave] = l;
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (lane == 0) s_l[wave] = l;
 #pragma unroll
-    for (int d = 0; d < D; ++d) s_o[wave][lane * D + d] = o[d];
-    __syncthreads();
-    if (tid < HD) {
-      const float lt = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-      const float ot = s_o[0][tid] + s_o[1][tid] + s_o[2][tid] + s_o[3][tid];
-      ((O *)a.out.p)[row * a.out.rs + head * a.out.hs + tid] = from_f<O>(lt == 0.0f ? 0.0f : ot / lt);
-      if (a.lse && tid == 0) a.lse[at] = lt == 0.0f ? -INFINITY : mm * kLn2 + logf(lt);
+      for (int d = 0; d < D; ++d) s_o[wave][lane * D + d] = o[d];
+      __syncthreads();
+      if (sub) continue;
+      l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) l += s_l[w];
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        o[d] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) o[d] += s_o[w][lane * D + d];
+      }
     }
+    if (head >= a.Hq) continue;
+    O *out = (O *)a.out.p + row * a.out.rs + head * a.out.hs + lane * D;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < D; ++d) out[d] = from_f<O>(o[d] * inv);
+    if (a.lse && lane == 0) a.lse[at] = l == 0.0f ? -INFINITY : mm * kLn2 + logf(l);
   }
 }
 
 // The kernel and the splits of a launch: query slots of a sequence and KV head
 // (rows * heads of its group) up to kFewSlots take the kernel above, more take
-// the one of k_qattn_rows.hip. Splits: enough workgroups to fill 256 CUs (four
-// each, or two of the larger ones), of at least 256 or 512 keys.
+// the one of k_qattn_rows.hip. Splits: those that take the fewest rounds of
+// resident workgroups (four on each of 256 CUs, or two of the larger ones) over
+// the keys of one, each workgroup counted as 256 or 512 keys longer than it is
+// (its queries, its results and their joining).
 constexpr int64_t kFewSlots = 32;
 struct Plan {
   bool few;
@@ -305,8 +322,20 @@ static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
   const bool few = slots <= kFewSlots;
   const int64_t block = few ? 16 : qattn_rows_block(c.hd), fill = few ? 1024 : 512, least = few ? 256 : 512;
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
-  const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
-  return {few, (int)std::max<int64_t>(1, std::min<int64_t>(most, (fill + units - 1) / units))};
+  if (few) {
+    const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
+    return {few, (int)std::max<int64_t>(1, std::min<int64_t>(most, (fill + units - 1) / units))};
+  }
+  Plan p = {few, 1};
+  int64_t best = INT64_MAX;
+  for (int n = 1; n <= kMaxSplit && (n == 1 || (n - 1) * least < len); ++n) {
+    const int64_t cost = (units * n + fill - 1) / fill * ((len + n - 1) / n + least);
+    if (cost < best) {
+      best = cost;
+      p.nsplit = n;
+    }
+  }
+  return p;
 }
 
 int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
@@ -314,9 +343,15 @@ int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
   return n == 1 ? 0 : (int64_t)b.n_rows * Hq * n * (c.hd + 2) * 4;
 }
 
+// One wave for each (row, head) where they are many (a launch of more waves
+// waits on their dispatch: 4 x 256 rows of 40 heads, 3 splits, 49 us with four),
+// four where there are many splits to read instead.
 template <typename O, int HD> static hipError_t run_join(const QAttn &a, int nsplit, hipStream_t st) {
   const unsigned rows = (unsigned)std::min(std::max(a.b.max_rows, 1), 65536);
-  hipLaunchKernelGGL((qattn_join_kernel<O, HD>), dim3(rows, a.Hq, a.b.n_seq), dim3(256), 0, st, a, nsplit);
+  if (nsplit <= 4)
+    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 1>), dim3(rows, (a.Hq + 3) / 4, a.b.n_seq), dim3(256), 0, st, a, nsplit);
+  else
+    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 4>), dim3(rows, a.Hq, a.b.n_seq), dim3(256), 0, st, a, nsplit);
   return hipGetLastError();
 }
 

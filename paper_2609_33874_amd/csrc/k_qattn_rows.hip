@@ -19,6 +19,12 @@
 namespace jetk {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+constexpr float kLag = 8.0f;  // a row's maximum is brought up to date when it lags by 2^8
+constexpr int kUnit = 7;      // probabilities are kept as p 2^7 <= 2^15
 
 // Work of a launch: units (sequence, KV head) of `per` workgroups each. The
 // workgroups of a unit run on one XCD (they share its keys in that L2), which
@@ -48,8 +54,9 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
   constexpr int RB = HD * 2, CPR = HD / 8;                // bytes and 16-byte chunks of an f16 row
   constexpr int PLANE = KT * RB, STAGE = 2 * PLANE;       // K, then V
   constexpr int RC = HD / 16, LD = KT * RC / (64 * NW);   // 16-byte chunks of an 8-bit row, and a thread's of a tile
-  extern __shared__ __align__(16) char smem[];
+  extern __shared__ __align__(1024) char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
   const int G = a.Hq / a.c.H, lb = a.c.lb;
   const int64_t units = OWN ? own.n_items : (int64_t)a.b.n_seq * a.c.H;
   const int per = OWN ? 1 : blocks * nsplit;
@@ -132,37 +139,38 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
         return own_tile(t.cs + n, t.cs + n);
       };
 
-      // 8-bit rows of a tile into registers (rows past its end: its last one),
-      // and the tile's scale bytes: lane l (mod 8) the one of K (l < 4) or V of
-      // keys 16 (l mod 4) ..
+      // 8-bit rows of a tile into registers, one after another as they lie (past
+      // its end: its last 16 bytes), and the tile's scale bytes: lane l (mod 8)
+      // the one of K (l < 4) or V of keys 16 (l mod 4) ..
       uint4 rk[LD], rv[LD];
       int re = 0;
+      const uint8_t *scales = lane & 4 ? VE : KE;
       auto load = [&](const Tile &t) {
-        const int tid = here(threadIdx.x), lane = tid & 63;
+        const uint8_t *kt = K + (int64_t)t.t0 * HD, *vt = V + (int64_t)t.t0 * HD;
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
-          const int x = i * 256 + tid;
-          const int64_t at = (int64_t)(t.t0 + min(x / RC, t.nk - 1)) * HD + x % RC * 16;
-          rk[i] = ld16(K + at);
-          rv[i] = ld16(V + at);
+          const uint32_t at = min(i * 4096 + (int)threadIdx.x * 16, t.nk * HD - 16);
+          rk[i] = ld16(kt + at);
+          rv[i] = ld16(vt + at);
         }
-        const int b = (t.t0 + min((lane & 3) * 16, t.nk - 1)) >> lb;
-        re = (lane & 4 ? VE : KE)[b];
+        re = scales[(t.t0 + min((here(threadIdx.x) & 3) * 16, t.nk - 1)) >> lb];
       };
-      // ... and from there into a stage
+      // ... and from there into a stage. (A thread's next chunk lies 4096 / HD
+      // rows on, where the swizzle is the same; chunks c and c + 1 of its 16
+      // values are neighbours in the swizzle too.)
       auto store = [&](int stage) {
-        char *dst = smem + stage * STAGE;
-        const int tid = here(threadIdx.x);
+        const int tid = here(threadIdx.x), r = tid / RC, c = tid % RC * 2;
+        const uint32_t at = lds0 + stage * STAGE + r * RB;
+        const uint32_t ka = at + ((c ^ kswz(r)) << 4), va = at + PLANE + ((c ^ vswz(r)) << 4);
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
-          const int x = i * 256 + tid, r = x / RC, c = x % RC * 2;
-          auto put = [&](char *row, int ca, int cb, const uint4 &u) {
+          auto put = [&](uint32_t to, const uint4 &u) {
             const uint2 p = f16x4_of<FMT>(u.x), q = f16x4_of<FMT>(u.y), s = f16x4_of<FMT>(u.z), t = f16x4_of<FMT>(u.w);
-            st16(row + ca * 16, make_uint4(p.x, p.y, q.x, q.y));
-            st16(row + cb * 16, make_uint4(s.x, s.y, t.x, t.y));
+            *(lds_u32x4 *)(uintptr_t)(to + i * (4096 / HD) * RB) = u32x4{p.x, p.y, q.x, q.y};
+            *(lds_u32x4 *)(uintptr_t)((to ^ 16) + i * (4096 / HD) * RB) = u32x4{s.x, s.y, t.x, t.y};
           };
-          put(dst + r * RB, c ^ kswz(r), (c + 1) ^ kswz(r), rk[i]);
-          put(dst + PLANE + r * RB, c ^ vswz(r), (c + 1) ^ vswz(r), rv[i]);
+          put(ka, rk[i]);
+          put(va, rv[i]);
         }
       };
       // 16-bit rows of an own tile straight into a stage
@@ -212,8 +220,8 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
       int ec = re, stage = 0;  // the current tile's scale bytes
       __syncthreads();         // the block before is done with the stages
       if (cur.nk > 0) {
-        if (cur.cs < 0) store(0);
-        else load_own(cur, 0);
+        if (!OWN || cur.cs < 0) store(0);
+        else if constexpr (OWN) load_own(cur, 0);
       }
       Tile ahead = next_tile(cur);
       if (ahead.nk > 0 && ahead.cs < 0) load(ahead);
@@ -223,34 +231,43 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
         const int ea = re;
         Tile after = ahead;
         if (ahead.nk > 0) {
-          if (ahead.cs < 0) store(stage ^ 1);
-          else load_own(ahead, stage ^ 1);
+          if (!OWN || ahead.cs < 0) store(stage ^ 1);
+          else if constexpr (OWN) load_own(ahead, stage ^ 1);
           after = next_tile(ahead);
-          if (after.nk > 0 && after.cs < 0) load(after);
+          if constexpr (OWN) {
+            if (after.nk > 0 && after.cs < 0) load(after);
+          } else {
+            load(after.nk > 0 ? after : ahead);  // (at the end the last tile again: no branch, no wait for it)
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
         if (!idle) {
-          const char *sk = smem + stage * STAGE, *sv = sk + PLANE;
           const int lane = here(threadIdx.x) & 63, g = lane >> 4, l16 = lane & 15;
+          // chunk 4 ks + g of key l16; the rest of a fragment's address is in its
+          // offset (stages and rows are powers of two: bits of ks flip in place)
+          const uint32_t ka = lds0 + stage * STAGE + l16 * RB + ((g ^ kswz(l16)) << 4);
+          // V transposed on the way out of LDS: lane l supplies 4 elements of
+          // key 4 g + (l % 16) / 4 and receives keys 4 g .. + 3 of dim l % 16
+          const int vr = 4 * g + (l16 >> 2);  // (16 and 32 rows on have the same swizzle)
+          const uint32_t va = lds0 + stage * STAGE + PLANE + vr * RB + (((l16 >> 1 & 1) ^ vswz(vr)) << 4) + (l16 & 1) * 8;
           const bool pre = !OWN || cur.cs < 0;
           f32x4 s[QB][4];
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
           auto read_k = [&](int ks, int kb) {
-            return ld16(sk + (kb * 16 + l16) * RB + (((ks * 4 + g) ^ kswz(l16)) << 4));
+            return *(const lds_u32x4 *)(uintptr_t)((ka ^ (ks << 6)) + kb * 16 * RB);
           };
-          auto score = [&](int ks, int kb, uint4 u) {
+          auto score = [&](int ks, int kb, u32x4 u) {
             Frag<f16> f;
             f.v = __builtin_bit_cast(f16x8, u);
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) mma16(s[qb][kb], f, qf[qb][ks]);
+            for (int qb = 0; qb < QB; ++qb) {
+              if (ks == 0) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+              mma16(s[qb][kb], f, qf[qb][ks]);
+            }
           };
           // fragments are read one group of products ahead, and no further (the
           // compiler would hold them all in registers)
           if (cur.nk > 48) {
-            uint4 f[2][4];
+            u32x4 f[2][4];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) f[0][kb] = read_k(0, kb);
 #pragma unroll
@@ -265,11 +282,15 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
             }
           } else {
 #pragma unroll
-            for (int kb = 0; kb < 3; ++kb)
-              if (kb * 16 < cur.nk) {
+            for (int kb = 0; kb < 4; ++kb) {
+              if (kb < 3 && kb * 16 < cur.nk) {
 #pragma unroll
                 for (int ks = 0; ks < NK; ++ks) score(ks, kb, read_k(ks, kb));
+              } else {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
               }
+            }
           }
           int ve[4], Mn = M;
           float ks2[4];
@@ -280,23 +301,31 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
             ve[kb] = pre ? __builtin_amdgcn_readlane(ec, 4 + kb) : kExpBias;
             Mn = max(Mn, v_top(ve[kb]));
           }
+          // V's scales, in units of 2^(Mn - 127), and whether all lie so close
+          // together that a probability may take them along (none NaN)
+          float vs[4];
+          bool near = true;
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) {
+            vs[kb] = v_scale(ve[kb], Mn);
+            near = near && vs[kb] >= 0x1p-60f;
+          }
+          const bool grown = Mn != M;
           const float unit = v_scale(M, Mn);
-          const bool same = ve[0] == Mn && ve[1] == Mn && ve[2] == Mn && ve[3] == Mn;
           M = Mn;
+          const bool seen = pre && cur.t0 + KT <= min(vis_min, key1);  // every key of the tile by every query
           Frag<f16> pf[QB][2];
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) {
-            float mx = -INFINITY;
-            if (pre && cur.t0 + KT <= min(vis_min, key1)) {
+            // z = s f, the largest z, and p = 2^(z - m): where all keys are
+            // seen z itself is not needed (f >= 0: largest z from largest s)
+            float f[4], mx = -INFINITY;
 #pragma unroll
-              for (int kb = 0; kb < 4; ++kb) {
-                const float f = ks2[kb] * fq[qb];
+            for (int kb = 0; kb < 4; ++kb) f[kb] = ks2[kb] * fq[qb];
+            if (seen) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  s[qb][kb][e] *= f;
-                  mx = fmaxf(mx, s[qb][kb][e]);
-                }
-              }
+              for (int kb = 0; kb < 4; ++kb)
+                mx = fmaxf(mx, f[kb] * fmaxf(fmaxf(s[qb][kb][0], s[qb][kb][1]), fmaxf(s[qb][kb][2], s[qb][kb][3])));
             } else {
               // last key of the tile that the query sees: the prefix's, or the
               // query's own row of its candidate's tile
@@ -304,42 +333,52 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
                                    : (first[qb] == cur.cs ? min(cur.nk - 1, row[qb] - cur.t0) : -1);
 #pragma unroll
               for (int kb = 0; kb < 4; ++kb) {
-                const float f = ks2[kb] * fq[qb];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                  const float z = kb * 16 + 4 * g + e <= last ? s[qb][kb][e] * f : -INFINITY;
+                  const float z = kb * 16 + 4 * g + e <= last ? s[qb][kb][e] * f[kb] : -INFINITY;
                   s[qb][kb][e] = z;
                   mx = fmaxf(mx, z);
                 }
+                f[kb] = 1.0f;
               }
             }
             mx = query_max(mx);
-            const float mn = fmaxf(m[qb], mx), ms = mn == -INFINITY ? 0.0f : mn, ms15 = ms - 15.0f;
-            const float al = __builtin_amdgcn_exp2f(m[qb] - ms);
-            m[qb] = mn;
+            // the accumulators are rescaled when some query's maximum lags too
+            // far behind (or their unit grew), not whenever one moves
+            if (grown || __any(mx > m[qb] + kLag)) {
+              const float mn = fmaxf(m[qb], mx), al = __builtin_amdgcn_exp2f(m[qb] - (mn == -INFINITY ? 0.0f : mn));
+              m[qb] = mn;
+              l[qb] *= al;
+#pragma unroll
+              for (int d = 0; d < ND; ++d) acc[qb][d] *= al * unit;
+            }
+            const float ms = (m[qb] == -INFINITY ? 0.0f : m[qb]) - (float)kUnit;
             float p[4][4], sum = 0.0f;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                p[kb][e] = __builtin_amdgcn_exp2f(s[qb][kb][e] - ms15);  // 2^15 p, and l in that unit
-                sum += p[kb][e];
-              }
-            l[qb] = l[qb] * al + sum;
-            if (!same) {
+            if (near) {
+              // p' = 2^(z - m + log2 vs), and l adds it up in p's own unit
 #pragma unroll
               for (int kb = 0; kb < 4; ++kb) {
-                const float f = v_scale(ve[kb], Mn);
+                const float mk = ms - (float)(ve[kb] - Mn);
+                float part = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)  // (a masked key's 0 must stay 0 where the scale is NaN)
-                  p[kb][e] = s[qb][kb][e] == -INFINITY ? 0.0f : p[kb][e] * f;
+                for (int e = 0; e < 4; ++e) {
+                  p[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][e], f[kb], -mk));
+                  part += p[kb][e];
+                }
+                sum = fmaf(part, pow2i(Mn - ve[kb]), sum);
               }
-            }
-            const float au = al * unit;
-            if (__any(au != 1.0f)) {
+            } else {
 #pragma unroll
-              for (int d = 0; d < ND; ++d) acc[qb][d] *= au;
+              for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float x = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][e], f[kb], -ms));
+                  sum += x;
+                  // (a masked key's 0 must stay 0 where the scale is NaN)
+                  p[kb][e] = !seen && s[qb][kb][e] == -INFINITY ? 0.0f : x * vs[kb];
+                }
             }
+            l[qb] += sum;
 #pragma unroll
             for (int mm = 0; mm < 2; ++mm) {
               const uint4 u = make_uint4(f2h2(p[2 * mm][0], p[2 * mm][1]), f2h2(p[2 * mm][2], p[2 * mm][3]),
@@ -348,17 +387,12 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
             }
             __builtin_amdgcn_sched_barrier(0);
           }
-          // V transposed on the way out of LDS: lane l supplies 4 elements of
-          // key 4 g + (l % 16) / 4 and receives keys 4 g .. + 3 of dim l % 16
 #pragma unroll
           for (int mm = 0; mm < 2; ++mm) {
             if (mm * 32 >= cur.nk) continue;
-            const int vr = 4 * g + (l16 >> 2);  // (16 and 32 rows on have the same swizzle)
-            const char *at = sv + (mm * 32 + vr) * RB + (l16 & 1) * 8;
             auto read_v = [&](int d, int half) {
-              const char *p = at + (((2 * d + (l16 >> 1 & 1)) ^ vswz(vr)) << 4) + half * 16 * RB;
-              typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-              return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_void *)p);
+              return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (lds_s16x4 *)(uintptr_t)((va ^ (d << 5)) + (mm * 32 + half * 16) * RB));
             };
             constexpr int DB = 4;
             s16x4 f[2][DB][2];
@@ -393,14 +427,14 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
 
       {
       const int lane = here(threadIdx.x) & 63, g = lane >> 4, l16 = lane & 15;
-      const float up = pow2i(max(M - kExpBias - 15, -126));
+      const float up = pow2i(max(M - kExpBias - kUnit, -126));
       const int64_t n = (int64_t)a.b.n_rows * a.Hq;
       const Parts parts = parts_of(a.ws, n, nsplit, HD);
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         float lt = l[qb] + __shfl_xor(l[qb], 16);
         lt += __shfl_xor(lt, 32);
-        lt *= 0x1p-15f;
+        lt *= pow2i(-kUnit);
         const int s = sb + (wave * QB + qb) * 16 + l16, head = h * G + s % G;
         if (s >= slots) continue;
         const int64_t row = row0 + s / G, at = row * a.Hq + head;

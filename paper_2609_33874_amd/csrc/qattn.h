@@ -6,9 +6,10 @@
 // sum of the softmax. The 8-bit values are exact in f16, so both products run
 // on the matrix cores in f16 with the scales outside of them: K's on the
 // scores, V's on the probabilities. A probability goes into the second product
-// as p 2^(ev - M) 2^15 in f16, M the largest V exponent met so far (the
-// accumulators are in units of 2^(M - 15) and rescaled when M grows), so that
-// what it loses is its rounding to 11 bits, or 2^-40 of the largest value.
+// as p 2^(ev - M) 2^u in f16, M the largest V exponent met so far (the
+// accumulators are in units of 2^(M - u) and rescaled when M grows), so that
+// what it loses is its rounding to 11 bits, or 2^-(25 + u) of the largest value
+// (u is 15, or 7 where p may reach 2^8).
 // bf16 queries enter as f16 times a power of two that puts a row's largest
 // value in [2^14, 2^15): exact down to 2^-30 of it.
 #pragma once
@@ -27,8 +28,9 @@ __device__ __host__ __forceinline__ Parts parts_of(void *ws, int64_t n, int nspl
   return {o, o + n * nsplit * hd, o + n * nsplit * (hd + 1)};
 }
 
-// Query q as f16 fragments: fragment ks holds elements at + ks * step .. + 7.
-// Returns what scores are multiplied by, up to the scales of K.
+// Query q as f16 fragments: fragment ks holds elements at + ks * step .. + 7,
+// with the sign of scale2. Returns what scores are multiplied by, up to the
+// scales of K (>= 0).
 template <typename T, int NK>
 __device__ __forceinline__ float load_query(Frag<f16> (&f)[NK], const T *q, int at, int step, bool vec, float scale2) {
   float x[NK][8];
@@ -50,13 +52,14 @@ __device__ __forceinline__ float load_query(Frag<f16> (&f)[NK], const T *q, int 
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[ks][j]) & 0x7fffffffu);
   }
-  float up = 1.0f;
+  float up = scale2 < 0.0f ? -1.0f : 1.0f;
+  scale2 = fabsf(scale2);
   if constexpr (__is_same(T, bf16)) {
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     // largest value 2^x f, f in [1, 2): times 2^(14 - x), and back on the scores
     const int e = min(max((int)(top >> 23) - 127, -112), 127);
-    if (top) up = pow2i(14 - e);
+    if (top) up *= pow2i(14 - e);
     if (top) scale2 *= pow2i(e - 14);
   }
 #pragma unroll

@@ -9,9 +9,10 @@ attention, for one output, with u = 2^-24 and the scores in 32 bits:
     probability then moves by the factor e^ds, and the weights p / l by e^2ds.
   * exp2 of a f32 difference, the sums over n keys and their rescaling: (n + 64) u
     relative (64: a rescaling for each of many splits, the exponential's own ulps)
-  * a probability is rounded to f16 (relative 2^-11), or below 2^-24 of f16's
-    range (its largest is kept at 2^15): 2^-40 of the largest scale met, a key;
-    the sum l is of the unrounded ones
+  * a probability is rounded to f16 (relative 2^-11), or to f16's least step: it
+    is kept as 2^u p with u = 15, or 7 where the maximum that it is relative to
+    may lag by 2^8, so half a step (2^-25) is at most 2^-32 of a probability of 1,
+    times the largest |v| met, a key; the sum l is of the unrounded ones
   * the output is rounded once: half a step of its type.
 """
 import sys
@@ -302,7 +303,7 @@ def check_attention(p, q, rows, causal, out="same", scale=None, lens=None, lse=T
             g = got[r:r + m, hs]
             ds = (hd + 6) * U * abs(scale) * qk[..., None]
             big = np.nanmax(np.abs(v)) if n else 0.0
-            tol = pv * (2 * np.expm1(np.minimum(ds, 1.0)) + (n + 64) * U + 2.0 ** -11) + n * 2.0 ** -40 * big * 2
+            tol = pv * (2 * np.expm1(np.minimum(ds, 1.0)) + (n + 64) * U + 2.0 ** -11) + n * 2.0 ** -32 * big * 2
             tol = tol + np.abs(want) * 1.01 * ref.half_step(otype) + torch.finfo(otype).tiny * ref.half_step(otype) * 2
             bad = np.isnan(want)
             np.testing.assert_array_equal(np.isnan(g), bad)
