@@ -11,7 +11,7 @@ namespace jetk {
 // ---------------------------------------------------------------------------
 
 constexpr int kTile = 32;    // keys of a wave's step
-constexpr int kWaves = 4;    // waves of a workgroup, on neighbouring tiles
+constexpr int kWaves = 8;    // waves of a workgroup, on neighbouring tiles
 constexpr int kMaxSplit = 128;
 
 template <int HD> struct QTile {
@@ -252,14 +252,15 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
 }
 
 // The splits' results of a (row of a sequence, query head) joined, by W waves:
-// every W-th split each, then added up in LDS. A workgroup takes 4 / W heads.
+// every W-th split each, then added up in LDS. A workgroup takes NH heads.
 // Rows of no sequence have no results and are left out.
-template <typename O, int HD, int W>
-__global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
-  constexpr int D = HD / 64, N = 4 / W;
-  __shared__ float s_l[4], s_o[4][HD];
+template <typename O, int HD, int W, int NH>
+__global__ __launch_bounds__(64 * W * NH) void qattn_join_kernel(QAttn a, int nsplit) {
+  static_assert(W == 1 || NH == 1, "heads share no LDS");
+  constexpr int D = HD / 64;
+  __shared__ float s_o[W][HD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave % W;
-  const int head = blockIdx.y * N + wave / W;
+  const int head = blockIdx.y * NH + wave / W;
   const QSeq sq = qseq(a.b, a.c, blockIdx.z);
   const int64_t n = (int64_t)a.b.n_rows * a.Hq;
   const Parts parts = parts_of(a.ws, n, nsplit, HD);
@@ -267,29 +268,42 @@ __global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
     const int64_t row = sq.row0 + i, at = row * a.Hq + head;
     float mm = -INFINITY, l = 0.0f, o[D] = {};
     if (head < a.Hq) {
-      // every wave finds the maximum over all splits
-      for (int s = lane; s < nsplit; s += 64) mm = fmaxf(mm, parts.m[s * n + at]);
-      mm = warp_max(mm);
-      const float ms = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll 8
-      for (int s = sub; s < nsplit; s += W) {
-        const float f = __builtin_amdgcn_exp2f(parts.m[s * n + at] - ms);
-        l += parts.l[s * n + at] * f;
-        const float *p = parts.o + (s * n + at) * HD + lane * D;
+      // every wave has all maxima and sums, one or two a lane (kMaxSplit 128)
+      float ms[2], ls[2];
 #pragma unroll
-        for (int d = 0; d < D; ++d) o[d] += p[d] * f;
+      for (int k = 0; k < 2; ++k) {
+        const int s = lane + 64 * k;
+        ms[k] = s < nsplit ? parts.m[s * n + at] : -INFINITY;
+        ls[k] = s < nsplit ? parts.l[s * n + at] : 0.0f;
+      }
+      mm = warp_max(fmaxf(ms[0], ms[1]));
+      const float base = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) ms[k] = __builtin_amdgcn_exp2f(ms[k] - base);  // the splits' weights
+      l = warp_sum(ls[0] * ms[0] + ls[1] * ms[1]);
+      for (int s0 = sub; s0 < nsplit; s0 += 8 * W) {  // eight splits' rows on their way at a time
+        float x[8][D];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float *p = parts.o + (min(s0 + k * W, nsplit - 1) * n + at) * HD + lane * D;
+#pragma unroll
+          for (int d = 0; d < D; ++d) x[k][d] = p[d];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int s = min(s0 + k * W, nsplit - 1);
+          const float f = s0 + k * W < nsplit ? __shfl(s < 64 ? ms[0] : ms[1], s & 63) : 0.0f;
+#pragma unroll
+          for (int d = 0; d < D; ++d) o[d] += f != 0.0f ? x[k][d] * f : 0.0f;
+        }
       }
     }
     if constexpr (W > 1) {
       __syncthreads();
-      if (lane == 0) s_l[wave] = l;
 #pragma unroll
       for (int d = 0; d < D; ++d) s_o[wave][lane * D + d] = o[d];
       __syncthreads();
       if (sub) continue;
-      l = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) l += s_l[w];
 #pragma unroll
       for (int d = 0; d < D; ++d) {
         o[d] = 0.0f;
@@ -306,12 +320,20 @@ __global__ __launch_bounds__(256) void qattn_join_kernel(QAttn a, int nsplit) {
   }
 }
 
-// The kernel and the splits of a launch: query slots of a sequence and KV head
+// The kernel and the splits of a launch. Query slots of a sequence and KV head
 // (rows * heads of its group) up to kFewSlots take the kernel above, more take
-// the one of k_qattn_rows.hip. Splits: those that take the fewest rounds of
-// resident workgroups (four on each of 256 CUs, or two of the larger ones) over
-// the keys of one, each workgroup counted as 256 or 512 keys longer than it is
-// (its queries, its results and their joining).
+// the one of k_qattn_rows.hip. Either needs about 512 workgroups, two on each
+// of 256 CUs.
+// Few slots: so many splits that there are 512 workgroups, of 512 keys at least
+// (two tiles a wave) and none up to 1024 keys, where the joining costs more: one
+// question's 731 keys 13.1 us with two splits, 10.9 with one. Twice as many
+// where that leaves 8192 keys each, so that sequences of different lengths do
+// not leave the GPU half empty at the end: 16 of 65536 .. 131072 keys 626 us with
+// 512 workgroups, 583 with 1024; but 64 of 1024 .. 4096 keys 76 and 82 (joining).
+// Many slots: the splits that take the fewest rounds of 512 workgroups over the
+// keys of one, each workgroup counted as 512 keys longer than it is (its
+// queries, its results and their joining): 320 workgroups of 4096 .. 8192 keys
+// take 289 us in 2 splits (640: two rounds, the second nearly empty), 220 in 3.
 constexpr int64_t kFewSlots = 32;
 struct Plan {
   bool few;
@@ -320,19 +342,22 @@ struct Plan {
 static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
   const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::max<int64_t>(b.max_len, 1);
   const bool few = slots <= kFewSlots;
-  const int64_t block = few ? 16 : qattn_rows_block(c.hd), fill = few ? 1024 : 512, least = few ? 256 : 512;
+  const int64_t block = few ? 16 : qattn_rows_block(c.hd), fill = 512, least = 512;
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
+  const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
   if (few) {
-    const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
-    return {few, (int)std::max<int64_t>(1, std::min<int64_t>(most, (fill + units - 1) / units))};
+    if (len <= 2 * least) return {few, 1};
+    int64_t n = std::min<int64_t>(most, (fill + units - 1) / units);
+    if (len / n >= 8192) n = std::min<int64_t>(most, (2 * fill + units - 1) / units);
+    return {few, (int)n};
   }
   Plan p = {few, 1};
   int64_t best = INT64_MAX;
-  for (int n = 1; n <= kMaxSplit && (n == 1 || (n - 1) * least < len); ++n) {
+  for (int64_t n = 1; n <= most; ++n) {
     const int64_t cost = (units * n + fill - 1) / fill * ((len + n - 1) / n + least);
     if (cost < best) {
       best = cost;
-      p.nsplit = n;
+      p.nsplit = (int)n;
     }
   }
   return p;
@@ -343,15 +368,15 @@ int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
   return n == 1 ? 0 : (int64_t)b.n_rows * Hq * n * (c.hd + 2) * 4;
 }
 
-// One wave for each (row, head) where they are many (a launch of more waves
-// waits on their dispatch: 4 x 256 rows of 40 heads, 3 splits, 49 us with four),
-// four where there are many splits to read instead.
+// One wave for each (row, head) of few splits, four of them a workgroup (4 x 256
+// rows of 40 heads, 3 splits: 27 us, 49 with four waves each); eight where there
+// are many splits to read.
 template <typename O, int HD> static hipError_t run_join(const QAttn &a, int nsplit, hipStream_t st) {
-  const unsigned rows = (unsigned)std::min(std::max(a.b.max_rows, 1), 65536);
-  if (nsplit <= 4)
-    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 1>), dim3(rows, (a.Hq + 3) / 4, a.b.n_seq), dim3(256), 0, st, a, nsplit);
+  const unsigned rows = (unsigned)std::min(std::max(a.b.max_rows, 1), 65536), n_seq = (unsigned)a.b.n_seq;
+  if (nsplit <= 8)
+    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 1, 4>), dim3(rows, (a.Hq + 3) / 4, n_seq), dim3(256), 0, st, a, nsplit);
   else
-    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 4>), dim3(rows, a.Hq, a.b.n_seq), dim3(256), 0, st, a, nsplit);
+    hipLaunchKernelGGL((qattn_join_kernel<O, HD, 8, 1>), dim3(rows, a.Hq, n_seq), dim3(512), 0, st, a, nsplit);
   return hipGetLastError();
 }
 

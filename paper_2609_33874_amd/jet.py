@@ -326,42 +326,56 @@ def jet_model_free(model) -> None:
 # `stream` (a raw hipStream_t), by default torch's current stream of that GPU.
 # ---------------------------------------------------------------------------
 
-def _device_array(t, name, dtype, device, shape=None, contiguous=True):
-    """Pointer of a torch tensor on `device` (None stays None)."""
+# These calls take about as long as their smallest kernels run: their checks are
+# written for few and cheap steps (devices as ordinals, shapes as they are).
+
+_torch = None  # (torch, float types -> JET_T_*, getter of a GPU's current raw stream), once imported
+
+
+def _t():
+    global _torch
+    if _torch is None:
+        import torch
+        types = {torch.float32: JET_T_F32, torch.float16: JET_T_F16, torch.bfloat16: JET_T_BF16}
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _torch = (torch, types, raw or (lambda i: torch.cuda.current_stream(i).cuda_stream))
+    return _torch
+
+
+def _device_array(t, name, dtype, device, shape=None):
+    """Pointer of a contiguous torch tensor on GPU `device` (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device:
-        raise TypeError(f"{name} must be {dtype} on {device}")
-    if contiguous and not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be {dtype} on cuda:{device}")
+    if not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
     return t.data_ptr() or None
 
 
 def _type_of(t, name):
-    import torch
-    ty = {torch.float32: JET_T_F32, torch.float16: JET_T_F16, torch.bfloat16: JET_T_BF16}.get(t.dtype)
+    ty = _t()[1].get(t.dtype)
     if ty is None:
         raise TypeError(f"{name} must be float32, float16 or bfloat16")
     return ty
 
 
 def _rows(t, name, heads, head_dim, device):
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim:
-        raise ValueError(f"{name} must have shape [rows, {heads}, {head_dim}], not {list(t.shape)}")
-    if t.device != device:
-        raise TypeError(f"{name} must be on {device}")
-    if t.stride(2) != 1:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
+        raise ValueError(f"{name} must have shape [rows, {heads}, {head_dim}], not {list(shape)}")
+    if t.get_device() != device:
+        raise TypeError(f"{name} must be on cuda:{device}")
+    rs, hs, es = t.stride()
+    if es != 1:
         raise TypeError(f"{name} must have its last dimension contiguous")
-    return jet_rows(t.data_ptr() or None, _type_of(t, name), 0, t.stride(0), t.stride(1))
+    return jet_rows(t.data_ptr() or None, _type_of(t, name), 0, rs, hs)
 
 
 def _stream(stream, device):
-    if stream is not None:
-        return stream
-    import torch
-    return torch.cuda.current_stream(device).cuda_stream
+    return _t()[2](device) if stream is None else stream
 
 
 class QCache:
@@ -370,7 +384,7 @@ class QCache:
     [heads, slots // block]. `QCache.empty` makes them."""
 
     def __init__(self, k, v, k_exp, v_exp, block: int = 32, format: int = JET_QCACHE_INT8):
-        import torch
+        torch = _t()[0]
         if k.dim() != 3 or k.element_size() != 1:
             raise TypeError("k must hold bytes, [heads, slots, head_dim]")
         H, S, hd = k.shape
@@ -381,11 +395,11 @@ class QCache:
         if not (k.is_contiguous() and v.is_contiguous()):
             raise TypeError("k and v must be contiguous")
         shape = (H, S // block if block > 0 else 0)
-        self.device = k.device
+        self.device = k.get_device()  # ordinal
         self.tensors = (k, v, k_exp, v_exp)
         self.c = jet_qcache(format, block, H, hd, S, k.data_ptr() or None, v.data_ptr() or None,
-                            _device_array(k_exp, "k_exp", torch.uint8, k.device, shape),
-                            _device_array(v_exp, "v_exp", torch.uint8, k.device, shape))
+                            _device_array(k_exp, "k_exp", torch.uint8, self.device, shape),
+                            _device_array(v_exp, "v_exp", torch.uint8, self.device, shape))
 
     @classmethod
     def empty(cls, heads: int, slots: int, head_dim: int, block: int = 32, format: int = JET_QCACHE_INT8,
@@ -397,26 +411,23 @@ class QCache:
 
 
 def _batch(cache, slot0, length, n_rows, row_offsets, max_rows, max_len):
-    import torch
-    n = slot0.shape[0]
-    if row_offsets is None:
-        off, most = None, 1
-    else:
-        off, most = _device_array(row_offsets, "row_offsets", torch.int32, cache.device, (n + 1,)), n_rows
-    return jet_qcache_batch(n, n_rows, most if max_rows is None else max_rows, 0,
-                            cache.c.n_slots if max_len is None else max_len,
-                            _device_array(slot0, "slot0", torch.int64, cache.device, (n,)),
-                            _device_array(length, "length", torch.int32, cache.device, (n,)), off)
+    torch, dev, n = _t()[0], cache.device, slot0.shape[0]
+    off = None if row_offsets is None else _device_array(row_offsets, "row_offsets", torch.int32, dev, (n + 1,))
+    if max_rows is None:
+        max_rows = 1 if off is None else n_rows
+    return jet_qcache_batch(n, n_rows, max_rows, 0, cache.c.n_slots if max_len is None else max_len,
+                            _device_array(slot0, "slot0", torch.int64, dev, (n,)),
+                            _device_array(length, "length", torch.int32, dev, (n,)), off)
 
 
 def _move_rows(fn, cache, slot0, length, k, v, row_offsets, max_rows, stream):
-    H, hd = cache.c.n_heads, cache.c.head_dim
-    rk, rv = _rows(k, "k", H, hd, cache.device), _rows(v, "v", H, hd, cache.device)
-    if k.shape[0] != v.shape[0]:
+    c, dev = cache.c, cache.device
+    H, hd = c.n_heads, c.head_dim
+    rk, rv, n = _rows(k, "k", H, hd, dev), _rows(v, "v", H, hd, dev), k.shape[0]
+    if n != v.shape[0]:
         raise ValueError("k and v have different numbers of rows")
-    b = _batch(cache, slot0, length, k.shape[0], row_offsets, max_rows, None)
-    _check(fn(ctypes.byref(cache.c), ctypes.byref(b), ctypes.byref(rk), ctypes.byref(rv),
-              _stream(stream, cache.device)))
+    # (structs are passed by reference: ctypes does that itself for a POINTER argument)
+    _check(fn(c, _batch(cache, slot0, length, n, row_offsets, max_rows, None), rk, rv, _stream(stream, dev)))
 
 
 def jet_qcache_write(cache: QCache, slot0, length, k, v, row_offsets=None, max_rows=None, stream=None) -> None:
@@ -448,27 +459,25 @@ def jet_qcache_attention(cache: QCache, slot0, length, q, out, row_offsets=None,
     each sequence; lse: float32 [rows, n_q_heads] or None. scale: 1 /
     sqrt(head_dim) by default. workspace: a uint8 tensor of at least
     jet_qcache_attention_workspace bytes (None: one is allocated). Returns out."""
-    import torch
-    dev, hd = cache.device, cache.c.head_dim
-    if q.dim() != 3 or out.shape != q.shape:
+    c, dev, L, torch = cache.c, cache.device, lib(), _t()[0]
+    hd, shape = c.head_dim, q.shape
+    if len(shape) != 3 or out.shape != shape:
         raise ValueError("q and out must have shape [rows, n_q_heads, head_dim]")
-    R, Hq = q.shape[0], q.shape[1]
+    R, Hq = shape[0], shape[1]
     rq, ro = _rows(q, "q", Hq, hd, dev), _rows(out, "out", Hq, hd, dev)
     b = _batch(cache, slot0, length, R, row_offsets, max_rows, max_len)
     st = _stream(stream, dev)
     if workspace is None:
         n = ctypes.c_int64()
-        _check(lib().jet_qcache_attention_workspace(ctypes.byref(cache.c), ctypes.byref(b), Hq, ctypes.byref(n)))
+        _check(L.jet_qcache_attention_workspace(c, b, Hq, n))
         if n.value:
-            workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+            workspace = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{dev}")
             if stream is not None:  # keep its memory until that stream's work is done
                 workspace.record_stream(torch.cuda.ExternalStream(stream, device=dev))
     ws, ws_n = (None, 0) if workspace is None else (_device_array(workspace, "workspace", torch.uint8, dev),
                                                     workspace.numel())
-    _check(lib().jet_qcache_attention(ctypes.byref(cache.c), ctypes.byref(b), Hq,
-                                      hd ** -0.5 if scale is None else scale, 1 if causal else 0, ctypes.byref(rq),
-                                      ctypes.byref(ro),
-                                      _device_array(lse, "lse", torch.float32, dev, (R, Hq)), ws, ws_n, st))
+    _check(L.jet_qcache_attention(c, b, Hq, hd ** -0.5 if scale is None else scale, 1 if causal else 0, rq, ro,
+                                  _device_array(lse, "lse", torch.float32, dev, (R, Hq)), ws, ws_n, st))
     return out
 
 
@@ -481,19 +490,23 @@ def jet_logits_adjust(logits, out=None, history=None, hist_prompt=None, repetiti
     frequency: float32 [rows]. bias: (offsets int32 [rows + 1], ids int32,
     values float32). masks: int32 [n_masks, words], bit v % 32 of word v / 32
     allows token v; mask_index: int32 [rows], < 0 for none. Returns out."""
-    import torch
+    torch = _t()[0]
     out = logits if out is None else out
-    if logits.dim() != 2 or out.shape != logits.shape or out.dtype != logits.dtype:
+    shape = logits.shape
+    if len(shape) != 2 or out.shape != shape or out.dtype is not logits.dtype:
         raise ValueError("logits and out must be [rows, vocab] of one type")
-    dev, (R, V) = logits.device, logits.shape
-    if not logits.is_cuda or out.device != dev:
+    R, V = shape
+    dev = logits.get_device()
+    if dev < 0 or out.get_device() != dev:
         raise TypeError("logits and out must be on one GPU")
-    if V > 1 and (logits.stride(1) != 1 or out.stride(1) != 1):
+    (ld, s1), (ld_out, o1) = logits.stride(), out.stride()
+    if V > 1 and (s1 != 1 or o1 != 1):
         raise TypeError("logits and out must have contiguous rows")
-    ld = lambda t: max(t.stride(0), V) if R <= 1 else t.stride(0)  # noqa: E731
+    if R <= 1:
+        ld, ld_out = max(ld, V), max(ld_out, V)
     i32, f32 = torch.int32, torch.float32
-    a = jet_logits_args(n_rows=R, vocab=V, type=_type_of(logits, "logits"), logits=logits.data_ptr() or None,
-                        out=out.data_ptr() or None, row_stride=ld(logits), out_stride=ld(out))
+    a = jet_logits_args(R, V, _type_of(logits, "logits"), 0, logits.data_ptr() or None, out.data_ptr() or None, ld,
+                        ld_out)
     if history is not None:
         a.hist_offsets = _device_array(history[0], "history offsets", i32, dev, (R + 1,))
         a.hist_ids, a.n_hist = _device_array(history[1], "history ids", i32, dev), history[1].numel()
@@ -511,5 +524,5 @@ def jet_logits_adjust(logits, out=None, history=None, hist_prompt=None, repetiti
         a.masks, a.n_masks = _device_array(masks, "masks", i32, dev), masks.shape[0]
         a.mask_stride = masks.shape[1]
     a.mask_index = _device_array(mask_index, "mask_index", i32, dev, (R,))
-    _check(lib().jet_logits_adjust(ctypes.byref(a), _stream(stream, dev)))
+    _check(lib().jet_logits_adjust(a, _stream(stream, dev)))
     return out
