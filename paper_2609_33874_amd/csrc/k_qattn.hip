@@ -48,13 +48,12 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // those same keys: a transposition of bytes inside the lane makes the A
 // operand, dim HD/16 c + i in product i.
 template <typename T, typename O, int FMT, int HD, int QB>
-__global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int nsplit) {
+__global__ __launch_bounds__(64 * kWaves, HD == 256 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit) {
   constexpr int ND = HD / 16, NK = HD / 32, LD = HD + 4;
   typedef QTile<HD> Tile;
   __shared__ float s_o[kWaves][16 * QB][LD];
   __shared__ float s_m[kWaves][16 * QB], s_l[kWaves][16 * QB];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y, G = a.Hq / a.c.H, sp = blockIdx.x % nsplit;
   const QSeq sq = qseq(a.b, a.c, blockIdx.z);
   const int slots = sq.n * G;
@@ -71,9 +70,37 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
     const int t1 = min(ntile, (sp + 1) * per);
     int t = sp * per + wave;
 
+    // (a tile's rows lie one after another; past the sequence's end its last
+    // row's bytes are loaded: those keys are masked)
+    const int last = sq.len - 1;
+    auto load_k = [&](Tile &x, int tile) {
+      const int k0 = tile * kTile, lane = here(threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
+      const uint8_t *p = K + (int64_t)k0 * HD;
+      const uint32_t end = (uint32_t)min(last - k0, kTile) * HD + (HD - HD / 4);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        load_words(x.k[kb], p + min((uint32_t)(c * HD + g * (HD / 4) + kb * 16 * HD), end));
+        x.ke[kb] = KE[min(k0 + kb * 16, last) >> a.c.lb];
+      }
+    };
+    auto load_v = [&](Tile &x, int tile) {
+      const int k0 = tile * kTile, lane = here(threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
+      const uint8_t *p = V + (int64_t)k0 * HD;
+      const uint32_t end = (uint32_t)min(last - k0, kTile) * HD + (HD - ND);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        load_words(x.v[i], p + min((uint32_t)(4 * g * HD + c * ND + ((i >> 2) * 16 + (i & 3)) * HD), end));
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) x.ve[kb] = VE[min(k0 + kb * 16, last) >> a.c.lb];
+    };
+
+    Tile cur;
+    if (t < t1) load_k(cur, t), load_v(cur, t);  // (the queries' way here is as long)
+
     int vis[QB], vis_min = kend;  // keys that this lane's queries see
     Frag<f16> qf[QB][NK];
     float fq[QB];
+    const int g = here(threadIdx.x) >> 4 & 3, c = here(threadIdx.x) & 15;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int slot = sb + qb * 16 + c, i = min(slot, slots - 1) / G, head = h * G + min(slot, slots - 1) % G;
@@ -86,23 +113,6 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) vis_min = min(vis_min, __shfl_xor(vis_min, o));
 
-    auto load = [&](Tile &x, int tile) {
-      const int k0 = tile * kTile, last = sq.len - 1;  // keys past the end load the last one (they are masked)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int64_t r = min(k0 + kb * 16 + c, last);
-        load_words(x.k[kb], K + r * HD + g * (HD / 4));
-        const int b = min(k0 + kb * 16, last) >> a.c.lb;
-        x.ke[kb] = KE[b];
-        x.ve[kb] = VE[b];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t r = min(k0 + (i >> 2) * 16 + 4 * g + (i & 3), last);
-        load_words(x.v[i], V + r * HD + c * ND);
-      }
-    };
-
     float m[QB], l[QB];
     f32x4 acc[QB][ND];
     int M = 0;  // V exponent byte of the accumulators' unit
@@ -113,28 +123,33 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
 #pragma unroll
       for (int d = 0; d < ND; ++d) acc[qb][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    Tile cur, nxt;
-    if (t < t1) load(cur, t);
     for (; t < t1; t += kWaves) {
-      if (t + kWaves < t1) load(nxt, t + kWaves);
       const int k0 = t * kTile;
       f32x4 s[QB][2];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) s[qb][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
+      for (int ks = 0; ks < NK; ++ks) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
           const uint2 lo = f16x4_of<FMT>(cur.k[kb][2 * ks]), hi = f16x4_of<FMT>(cur.k[kb][2 * ks + 1]);
           Frag<f16> kf;
           kf.v = __builtin_bit_cast(f16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) mma16(s[qb][kb], kf, qf[qb][ks]);
         }
+        if (ks & 1) __builtin_amdgcn_sched_barrier(0);  // (not all of K as f16 at once: registers)
       }
+      // K's registers take the next tile's as soon as they are used, and V's
+      // later: a second tile in registers would leave room for half the waves
       const int ke0 = __builtin_amdgcn_readfirstlane(cur.ke[0]), ke1 = __builtin_amdgcn_readfirstlane(cur.ke[1]);
       const int ve0 = __builtin_amdgcn_readfirstlane(cur.ve[0]), ve1 = __builtin_amdgcn_readfirstlane(cur.ve[1]);
       const float ks2[2] = {k_scale(ke0), k_scale(ke1)};
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(cur, min(t + kWaves, t1 - 1));
+      __builtin_amdgcn_sched_barrier(0);
       const int Mn = max(M, max(v_top(ve0), v_top(ve1)));
       const float vs[2] = {v_scale(ve0, Mn), v_scale(ve1, Mn)}, unit = v_scale(M, Mn);
       M = Mn;
@@ -189,19 +204,21 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) mma16(acc[qb][4 * w + b], vf, pf[qb]);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      cur = nxt;
+      load_v(cur, min(t + kWaves, t1 - 1));
     }
 
     // the waves' results in LDS, in units of 1
+    const int tid = here(threadIdx.x), go = tid >> 4 & 3, co = tid & 15;
     const float up = pow2i(max(M - kExpBias - 15, -126));
     __syncthreads();  // the last block's have been read
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float lt = l[qb] + __shfl_xor(l[qb], 16);
       lt += __shfl_xor(lt, 32);
-      const int q = qb * 16 + c;
-      if (g == 0) {
+      const int q = qb * 16 + co;
+      if (go == 0) {
         s_m[wave][q] = m[qb];
         s_l[wave][q] = lt * 0x1p-15f;
       }
@@ -211,7 +228,7 @@ __global__ __launch_bounds__(64 * kWaves) void qattn_split_kernel(QAttn a, int n
 #pragma unroll
         for (int i = 0; i < ND; i += 4) {
           const f32x4 o = {acc[qb][i][e] * up, acc[qb][i + 1][e] * up, acc[qb][i + 2][e] * up, acc[qb][i + 3][e] * up};
-          *reinterpret_cast<f32x4 *>(&s_o[wave][q][ND * (4 * g + e) + i]) = o;
+          *reinterpret_cast<f32x4 *>(&s_o[wave][q][ND * (4 * go + e) + i]) = o;
         }
     }
     __syncthreads();

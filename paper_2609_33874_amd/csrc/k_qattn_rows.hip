@@ -39,14 +39,6 @@ __device__ __forceinline__ Work work_of(int64_t w, int64_t units, int per) {
   return {w / 8 / per * 8 + w % 8, (int)(w / 8 % per)};
 }
 
-// A thread's index that the compiler takes for a new value at each place: what
-// is computed from it stays inside the loop (moved out of it, the addresses of
-// a whole tile took registers that the accumulators need).
-__device__ __forceinline__ int here(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
 __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAttn a, OwnRows own, int blocks,
                                                                            int nsplit) {

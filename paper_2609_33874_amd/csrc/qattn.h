@@ -28,6 +28,14 @@ __device__ __host__ __forceinline__ Parts parts_of(void *ws, int64_t n, int nspl
   return {o, o + n * nsplit * hd, o + n * nsplit * (hd + 1)};
 }
 
+// A thread's index that the compiler takes for a new value at each place: what
+// is computed from it stays inside the loop (moved out of it, the addresses of
+// a whole tile took registers that the accumulators need).
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Query q as f16 fragments: fragment ks holds elements at + ks * step .. + 7,
 // with the sign of scale2. Returns what scores are multiplied by, up to the
 // scales of K (>= 0).
