@@ -76,10 +76,18 @@ enum { JET_CHOICE = 0, JET_BINARY = 1, JET_ORDINAL = 2 }; /* decision rule */
 /* flags for jet_load_opts.flags */
 enum {
   JET_FLAG_KERNEL_TIMING = 1, /* time every launch with HIP events (jet_stats) */
-  JET_FLAG_RECORD_ROUTES = 2  /* mixture-of-experts models: keep the experts each
+  JET_FLAG_RECORD_ROUTES = 2, /* mixture-of-experts models: keep the experts each
                                  layer chose for each row (jet_routes_get);
                                  a diagnostic for checking routing, it
                                  synchronises the stream at every such layer */
+  /* Retained attention caches in 8 bits (at most one of the two; JET_F16 and
+   * JET_FP32 modes, head_dim 64 or 128): a prefill attends to its own keys as
+   * they are and then keeps them as a jet_qcache does (blocks of 32 tokens);
+   * scoring and traces read them there, candidates' own keys stay in the mode's
+   * type. Half a JET_F16 prefix's bytes. In JET_FP32 the caches are read back
+   * into 32-bit rows for each call (validation). */
+  JET_FLAG_QCACHE_INT8 = 4,
+  JET_FLAG_QCACHE_E4M3 = 8
 };
 
 typedef struct jet_model jet_model;
@@ -192,6 +200,35 @@ int jet_prefill_prefix(jet_model *model, int32_t n_q, const int64_t *prefix_offs
  */
 int jet_generate_trace(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature, uint64_t seed,
                        int32_t *out_tokens);
+
+/* Rules for the tokens of a trace (see jet_logits_adjust, whose arithmetic they
+ * have). All arrays are host memory; questions and steps are numbered as in
+ * jet_generate_trace. The history of question q at step t is its context (none
+ * without context_offsets) and its t tokens so far; presence and frequency
+ * count the latter alone. */
+typedef struct {
+  float repetition;           /* > 0; 1: no penalty */
+  float presence, frequency;  /* finite; 0: no penalty */
+  int32_t n_masks;
+  const int64_t *context_offsets; /* int64[n_q + 1] or NULL */
+  const int32_t *context_tokens;  /* int32[context_offsets[n_q]], e.g. the prefixes */
+  const int64_t *bias_offsets;    /* int64[n_q + 1] or NULL */
+  const int32_t *bias_tokens;     /* token ids, and what is added to their logits (finite) */
+  const float *bias_values;
+  const uint32_t *masks;          /* uint32[n_masks][ceil(vocab / 32)] or NULL: bit v % 32 of
+                                     word v / 32 allows token v; each allows some token */
+  const int32_t *mask_index;      /* int32[n_q][n_steps]: the step's mask, < 0: any token.
+                                     Needed when masks are given */
+} jet_trace_rules;
+
+/*
+ * jet_generate_trace_rules - jet_generate_trace with rules: the logits of every
+ * step are adjusted before its token is sampled. rules NULL: none.
+ * Errors: as jet_generate_trace; JET_E_INVALID also for malformed rules
+ *   (nothing has changed then).
+ */
+int jet_generate_trace_rules(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature, uint64_t seed,
+                             const jet_trace_rules *rules, int32_t *out_tokens);
 
 /*
  * jet_score_candidates - teacher-forced log-likelihood of every candidate

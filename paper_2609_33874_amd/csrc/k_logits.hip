@@ -62,7 +62,8 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
   const int32_t *hp = HIST ? a.h_off + r : kNone, *bp = BIAS ? a.b_off + r : kNone;
   const int32_t *pp = HIST && a.h_prompt ? a.h_prompt + r : kNone, *ip = a.mask_index ? a.mask_index + r : kNone;
   const float *rp = a.rep ? a.rep + r : &kOne, *sp = a.pres ? a.pres + r : &kZero, *fp = a.freq ? a.freq + r : &kZero;
-  int h0 = hp[0], h1 = hp[1], b0 = bp[0], b1 = bp[1];
+  const int32_t *ep = HIST && a.h_end ? a.h_end + r : hp + 1;
+  int h0 = hp[0], h1 = ep[0], b0 = bp[0], b1 = bp[1];
   const int prompt = pp[0], index = ip[0];
   const RowRules w = {*rp, 1.0f / *rp, *sp, *fp};
   if (h0 < 0 || h1 < h0 || h1 > a.n_hist) h0 = h1 = 0;
@@ -250,6 +251,7 @@ hipError_t launch_logits_adjust(const LogitsArgs &a, hipStream_t st) {
     b.in = (const char *)a.in + (int64_t)r0 * a.in_ld * es;
     b.out = (char *)a.out + (int64_t)r0 * a.out_ld * es;
     if (b.h_off) b.h_off += r0;
+    if (b.h_end) b.h_end += r0;
     if (b.h_prompt) b.h_prompt += r0;
     if (b.rep) b.rep += r0;
     if (b.pres) b.pres += r0;

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
       auto load_own = [&](const Tile &t, int stage) {
         constexpr int RPL = 64 / CPR;  // rows of a wave's load
         char *dst = smem + stage * STAGE;
-        const f16 *Ko = own.K + (int64_t)h * own.s_suf * HD, *Vo = own.V + (int64_t)h * own.s_suf * HD;
+        const f16 *Ko = (const f16 *)own.K + (int64_t)h * own.s_suf * HD, *Vo = (const f16 *)own.V + (int64_t)h * own.s_suf * HD;
 #pragma unroll
         for (int i = 0; i < KT / RPL / NW; ++i) {
           const int blk = i * NW + wave, r = blk * RPL + lane / CPR, c = lane % CPR;
@@ -336,9 +336,12 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
             }
             mx = query_max(mx);
             // the accumulators are rescaled when some query's maximum lags too
-            // far behind (or their unit grew), not whenever one moves
-            if (grown || __any(mx > m[qb] + kLag)) {
-              const float mn = fmaxf(m[qb], mx), al = __builtin_amdgcn_exp2f(m[qb] - (mn == -INFINITY ? 0.0f : mn));
+            // far behind (or their unit grew), not whenever one moves; each query
+            // by its own maximum alone, whatever the others in its wave do
+            const bool lags = mx > m[qb] + kLag;
+            if (grown || __any(lags)) {
+              const float mn = lags ? mx : m[qb];
+              const float al = lags ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
               m[qb] = mn;
               l[qb] *= al;
 #pragma unroll
@@ -493,6 +496,16 @@ template <typename T, typename O> static hipError_t rows_fmt(const QAttn &a, int
 hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st) {
   if (a.q.type == 1) return a.out.type == 0 ? rows_fmt<f16, float>(a, nsplit, st) : rows_fmt<f16, f16>(a, nsplit, st);
   return a.out.type == 0 ? rows_fmt<bf16, float>(a, nsplit, st) : rows_fmt<bf16, bf16>(a, nsplit, st);
+}
+
+hipError_t launch_qattn_own(const QAttn &a, const OwnRows &own, hipStream_t st) {
+  if (own.n_items <= 0) return hipSuccess;
+  if (a.q.type != 1 || a.out.type != 1) return hipErrorInvalidValue;
+  if (a.c.hd == 64)
+    return a.c.fmt == 0 ? run_rows<f16, f16, 0, 64, 2, true>(a, own, 1, st) : run_rows<f16, f16, 1, 64, 2, true>(a, own, 1, st);
+  if (a.c.hd == 128)
+    return a.c.fmt == 0 ? run_rows<f16, f16, 0, 128, 2, true>(a, own, 1, st) : run_rows<f16, f16, 1, 128, 2, true>(a, own, 1, st);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace jetk

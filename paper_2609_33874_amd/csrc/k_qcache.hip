@@ -173,4 +173,34 @@ hipError_t launch_qcache_read(const QCache &c, const QBatch &b, const QRows &k, 
   return read_t<bf16>(c, b, k, v, st);
 }
 
+// One workgroup per (block of a sequence, head of K or of V, sequence): 16-byte
+// pieces of whole blocks and their scale bytes.
+__global__ __launch_bounds__(256) void qcache_copy_kernel(QCache s, QCache d, const int64_t *__restrict__ s0,
+                                                          const int64_t *__restrict__ d0, const int32_t *__restrict__ len) {
+  const int h = blockIdx.y >> 1, q = blockIdx.z;
+  const bool isv = blockIdx.y & 1;
+  const int blocks = (len[q] + (1 << s.lb) - 1) >> s.lb, n = (s.hd << s.lb) / 16;
+  const int64_t sb = s0[q] >> s.lb, db = d0[q] >> d.lb;
+  for (int b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const uint4 *from = (const uint4 *)((isv ? s.v : s.k) + ((int64_t)h * s.S + ((sb + b) << s.lb)) * s.hd);
+    uint4 *to = (uint4 *)((isv ? d.v : d.k) + ((int64_t)h * d.S + ((db + b) << d.lb)) * d.hd);
+    for (int i = threadIdx.x; i < n; i += 256) to[i] = from[i];
+    if (threadIdx.x == 0)
+      (isv ? d.ve : d.ke)[(int64_t)h * (d.S >> d.lb) + db + b] = (isv ? s.ve : s.ke)[(int64_t)h * (s.S >> s.lb) + sb + b];
+  }
+}
+
+hipError_t launch_qcache_copy(const QCache &src, const QCache &dst, const int64_t *src_slot0, const int64_t *dst_slot0,
+                              const int32_t *len, int n_seq, hipStream_t st) {
+  if (src.H != dst.H || src.hd != dst.hd || src.lb != dst.lb || src.fmt != dst.fmt) return hipErrorInvalidValue;
+  for (int q = 0; q < n_seq; q += 65535) {
+    const int n = std::min(n_seq - q, 65535);
+    hipLaunchKernelGGL(qcache_copy_kernel, dim3(64, 2 * src.H, n), dim3(256), 0, st, src, dst, src_slot0 + q, dst_slot0 + q,
+                       len + q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace jetk

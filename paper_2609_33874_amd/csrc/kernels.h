@@ -294,6 +294,23 @@ struct QAttn {
 };
 int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq);
 hipError_t launch_qattn(const QAttn &a, hipStream_t st);
+// Candidate scoring: f16 queries of body rows over their question's prefix in
+// the cache (a.c; a.q, a.out, a.Hq and a.scale as above, a.b unused) and the
+// body rows of their own candidate, as AttnArgs of mode 1 describes them.
+struct OwnRows {
+  const AttnItem *items;  // of at most qattn_rows_block(hd) query slots
+  AttnQuestions qs;
+  const void *K, *V;      // f16 [H][s_suf][hd]
+  int64_t s_suf;
+  const int32_t *row_n, *row_t;
+  int n_items;
+};
+int qattn_rows_block(int hd);
+hipError_t launch_qattn_own(const QAttn &a, const OwnRows &own, hipStream_t st);
+// Sequences' blocks [0, len) from one cache into another of the same form:
+// slot0 in either (device, [n_seq]).
+hipError_t launch_qcache_copy(const QCache &src, const QCache &dst, const int64_t *src_slot0, const int64_t *dst_slot0,
+                              const int32_t *len, int n_seq, hipStream_t st);
 
 // ---- logits of a decode step (k_logits.hip) ----
 struct LogitsArgs {
@@ -303,6 +320,7 @@ struct LogitsArgs {
   int64_t in_ld, out_ld;
   const int32_t *h_off, *h_ids, *h_prompt;
   int n_hist;
+  const int32_t *h_end;  // ends of the rows' histories, or NULL: h_off + 1
   const float *rep, *pres, *freq;
   const int32_t *b_off, *b_ids;
   const float *b_val;

@@ -97,4 +97,46 @@ Status check_logits(const jet_logits_args *a) {
   return Status::ok();
 }
 
+Status check_rules(const jet_trace_rules *r, int32_t n_q, int32_t n_steps, int64_t vocab) {
+  if (!r) return Status::ok();
+  if (!(r->repetition > 0.0f) || !std::isfinite(r->repetition) || !std::isfinite(1.0f / r->repetition))
+    return bad("repetition must be > 0 and finite, its inverse too");
+  if (!std::isfinite(r->presence) || !std::isfinite(r->frequency)) return bad("presence and frequency must be finite");
+  Status s;
+  if (r->context_offsets) {
+    s = check_offsets(r->context_offsets, n_q, 0, "context_offsets");
+    if (!s) return s;
+    if (r->context_offsets[n_q] > INT32_MAX) return bad("too many context tokens");
+    s = check_ids_host(r->context_tokens, r->context_offsets[n_q], vocab, "context_tokens");
+    if (!s) return s;
+  }
+  if (r->bias_offsets) {
+    s = check_offsets(r->bias_offsets, n_q, 0, "bias_offsets");
+    if (!s) return s;
+    const int64_t n = r->bias_offsets[n_q];
+    if (n > (1 << 30)) return bad("too many biases");
+    s = check_ids_host(r->bias_tokens, n, vocab, "bias_tokens");
+    if (!s) return s;
+    if (n > 0 && !r->bias_values) return bad("bias_values is NULL");
+    for (int64_t i = 0; i < n; ++i)
+      if (!std::isfinite(r->bias_values[i])) return bad("bias " + std::to_string(i) + " is not finite");
+  }
+  if (r->n_masks < 0) return bad("n_masks must be >= 0");
+  if (r->n_masks > 0) {
+    if (!r->masks || !r->mask_index) return bad("masks or mask_index is NULL");
+    const int64_t words = (vocab + 31) / 32;
+    for (int32_t m = 0; m < r->n_masks; ++m) {
+      uint32_t any = 0;
+      for (int64_t w = 0; w < words; ++w) {
+        const uint32_t x = r->masks[(int64_t)m * words + w];
+        any |= w == words - 1 && vocab % 32 ? x & ((1u << (vocab % 32)) - 1) : x;
+      }
+      if (!any) return bad("mask " + std::to_string(m) + " allows no token");
+    }
+    for (int64_t i = 0; i < (int64_t)n_q * n_steps; ++i)
+      if (r->mask_index[i] >= r->n_masks) return bad("mask_index " + std::to_string(i) + " names no mask");
+  }
+  return Status::ok();
+}
+
 }  // namespace jet

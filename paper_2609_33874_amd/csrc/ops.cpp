@@ -130,7 +130,7 @@ Status logits(const jet_logits_args *a, hipStream_t st) {
   OnDeviceOf dev(a->out, st);
   TRY(dev.st);
   const jetk::LogitsArgs l{a->n_rows,     a->vocab,       a->type,         a->n_masks,   a->logits,       a->out,
-                           a->row_stride, a->out_stride,  a->hist_offsets, a->hist_ids,  a->hist_prompt,  (int)a->n_hist,
+                           a->row_stride, a->out_stride,  a->hist_offsets, a->hist_ids,  a->hist_prompt,  (int)a->n_hist, nullptr,
                            a->repetition, a->presence,    a->frequency,    a->bias_offsets, a->bias_ids,  a->bias_values,
                            (int)a->n_bias, a->masks,      a->mask_stride,  a->mask_index};
   return launched(jetk::launch_logits_adjust(l, st), "jet_logits_adjust");

@@ -95,22 +95,8 @@ __device__ __forceinline__ float v_scale(int e, int M) {
 }
 __device__ __forceinline__ int v_top(int e) { return e == kExpNaN ? 0 : e; }
 
-// Candidate scoring (k_qattn_rows.hip): queries of body rows over their
-// question's prefix in the cache and the body rows of their own candidate in
-// f16, as AttnArgs of mode 1 (kernels.h) describes them.
-struct OwnRows {
-  const AttnItem *items;
-  AttnQuestions qs;
-  const f16 *K, *V;  // [H][s_suf][hd]
-  int64_t s_suf;
-  const int32_t *row_n, *row_t;
-  int n_items;
-};
-
-// Launches of the kernels for few and for many query slots (rows * heads of a
-// KV head's group) per sequence; the latter needs no workspace when nsplit is 1.
-int qattn_rows_block(int hd);
+// The kernel of k_qattn_rows.hip on a batch (needs no workspace when nsplit is
+// 1).
 hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st);
-hipError_t launch_qattn_own(const QAttn &a, const OwnRows &own, hipStream_t st);
 
 }  // namespace jetk

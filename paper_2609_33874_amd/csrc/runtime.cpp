@@ -9,6 +9,8 @@
 // log-probabilities (Eq. 3).
 #include "runtime.h"
 
+#include "op_checks.h"
+
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -509,6 +511,16 @@ Status load_model(jet_model *m, const char *path, const jet_load_opts *o) {
   TRY(read_model_header(m->path, &m->h));
   const ModelHeader &h = m->h;
   TRY(check_shapes(h, m->dtype));
+  const int qflags = m->flags & (JET_FLAG_QCACHE_INT8 | JET_FLAG_QCACHE_E4M3);
+  if (qflags) {
+    if (qflags == (JET_FLAG_QCACHE_INT8 | JET_FLAG_QCACHE_E4M3))
+      return Status::err(JET_E_INVALID, "a cache in 8 bits has one format: JET_FLAG_QCACHE_INT8 or _E4M3");
+    if (m->dtype != JET_F16 && m->dtype != JET_FP32)
+      return Status::err(JET_E_INVALID, "caches in 8 bits need the JET_F16 or the JET_FP32 mode");
+    if ((h.head_dim != 64 && h.head_dim != 128) || h.n_heads / h.n_kv_heads > 64)
+      return Status::err(JET_E_INVALID, "caches in 8 bits need head_dim 64 or 128 and at most 64 query heads a KV head");
+    m->qfmt = qflags == JET_FLAG_QCACHE_INT8 ? JET_QCACHE_INT8 : JET_QCACHE_E4M3;
+  }
   m->kdt = m->dtype == JET_FP32 ? 1 : (m->dtype == JET_F16 || m->dtype == JET_F16P) ? 2 : 0;
   m->edt = m->kdt == 1 ? 1 : 0;
   m->pair = m->dtype == JET_BF16 ? 1 : 0;
@@ -695,7 +707,8 @@ struct AttnPlan {
   double flops = 0, bytes = 0;
 };
 
-Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, AttnPlan *pl) {
+// own_cache: items for launch_qattn_own (the prefix keys in 8 bits).
+Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, AttnPlan *pl, bool own_cache = false) {
   const ModelHeader &h = m->h;
   const int G = (int)(h.n_heads / h.n_kv_heads);
   std::vector<jetk::AttnItem> items;
@@ -703,7 +716,9 @@ Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, 
   double slots = 0, nq = 0;
   for (auto n : qd.nrows)
     if (n > 0) slots += (double)G * n, nq += 1;
-  const int block = jetk::attn_block(m->kdt, m->apair, mode, nq > 0 ? slots / nq : 0, slots * (double)h.n_kv_heads);
+  const int block = own_cache
+                        ? jetk::qattn_rows_block((int)h.head_dim)
+                        : jetk::attn_block(m->kdt, m->apair, mode, nq > 0 ? slots / nq : 0, slots * (double)h.n_kv_heads);
   build_items(qd, G, (int)h.n_kv_heads, mode == 0, block, &items, &pairs);
   // Longest work first: the dispatcher hands out workgroups in order, so long
   // items no longer run alone at the end (an item's result does not depend
@@ -746,8 +761,9 @@ Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, 
   for (size_t q = 0; q < qd.nrows.size(); ++q)
     if (qd.nrows[q] > 0) kv_rows += (double)qd.pre_len[q] + (double)qd.suf_len[q];
   for (auto n : qd.nrows) qo_rows += n;
-  pl->bytes = (double)m->esz * m->anp * (kv_rows * 2.0 * (double)h.n_kv_heads * (double)h.head_dim +
-                                        qo_rows * 2.0 * (double)h.n_heads * (double)h.head_dim);
+  const double esz = (double)m->esz * m->anp;
+  pl->bytes = (own_cache ? 1.0 : esz) * kv_rows * 2.0 * (double)h.n_kv_heads * (double)h.head_dim +
+              esz * qo_rows * 2.0 * (double)h.n_heads * (double)h.head_dim;
   pl->flops = 4.0 * pairs * (double)h.head_dim;
   return Status::ok();
 }
@@ -776,6 +792,87 @@ Status run_attention(jet_model *m, AttnPlan &pl, const void *Q, int64_t R, void 
   KTimer t(m, cls >= 0 ? cls : a.mode == 0 ? JET_K_ATTN_PREFIX : JET_K_ATTN_CAND, pl.flops, pl.bytes);
   LAUNCH(jetk::launch_attention(m->kdt, a, m->st));
   return Status::ok();
+}
+
+// ---------------------------------------------------------------------------
+// retained attention caches in 8 bits (JET_FLAG_QCACHE_*)
+// ---------------------------------------------------------------------------
+
+constexpr int kQBlock = 32;     // tokens that share a scale
+constexpr int kMaxSeqs = 65535;  // sequences of a launch
+
+int64_t q_slots(int64_t len) { return (len + kQBlock - 1) / kQBlock * kQBlock; }
+
+jetk::QCache qcache_view(const jet_model *m, void *k, void *v, uint8_t *ke, uint8_t *ve, int64_t slots) {
+  return {m->qfmt, 5, (int)m->h.n_kv_heads, (int)m->h.head_dim, slots, (uint8_t *)k, (uint8_t *)v, ke, ve};
+}
+jetk::QCache qcache_of(const jet_model *m, const jet_prefix *p, int64_t l) {
+  return qcache_view(m, p->kcache[(size_t)l], p->vcache[(size_t)l], p->kexp[(size_t)l], p->vexp[(size_t)l],
+                     p->qslot0.back());
+}
+
+// Device tables of a call's sequences: slot0[n], len[n], rows[n + 1].
+struct QTables {
+  jetk::QBatch b{};
+  std::vector<int64_t> slot0;
+  std::vector<int32_t> len, rows;
+};
+Status upload_batch(jet_model *m, const char *tag, QTables *t) {
+  const std::string s(tag);
+  int64_t *d_slot0;
+  int32_t *d_len, *d_rows;
+  TRY(upload(m, (s + "slot0").c_str(), t->slot0, &d_slot0));
+  TRY(upload(m, (s + "len").c_str(), t->len, &d_len));
+  TRY(upload(m, (s + "rows").c_str(), t->rows, &d_rows));
+  int most = 0, longest = 0;
+  for (size_t i = 0; i < t->len.size(); ++i) {
+    most = std::max(most, t->rows[i + 1] - t->rows[i]);
+    longest = std::max(longest, t->len[i]);
+  }
+  // (in several launches, attention splits no keys: its workspace is sized for
+  // the rows of one)
+  if (t->len.size() > (size_t)kMaxSeqs) longest = 1;
+  t->b = {(int)t->len.size(), t->rows.back(), most, longest, d_slot0, d_len, d_rows};
+  return Status::ok();
+}
+// f on the batch's sequences, as many at a time as a launch takes.
+template <typename F> Status each_batch(const jetk::QBatch &b, F f) {
+  for (int q = 0; q < b.n_seq; q += kMaxSeqs) {
+    jetk::QBatch c = b;
+    c.n_seq = std::min(b.n_seq - q, kMaxSeqs);
+    c.slot0 += q;
+    c.len += q;
+    c.rows += q;
+    LAUNCH(f(c));
+  }
+  return Status::ok();
+}
+// Rows of [Hkv][R][hd] in the compute type.
+jetk::QRows kv_rows(const jet_model *m, void *p, int64_t R) {
+  return {p, m->kdt == 1 ? 0 : 1, 1, m->h.head_dim, R * m->h.head_dim};
+}
+double kv_bytes_of(const jet_model *m, int64_t rows, double per) {
+  return 2.0 * (double)rows * (double)(m->h.n_kv_heads * m->h.head_dim) * per;
+}
+
+Status qcache_write(jet_model *m, const jetk::QCache &c, const QTables &t, void *k, void *v, int64_t R) {
+  KTimer tm(m, JET_K_OTHER, 0, kv_bytes_of(m, R, (double)m->esz + 1.0));
+  return each_batch(t.b, [&](const jetk::QBatch &b) {
+    return jetk::launch_qcache_write(c, b, kv_rows(m, k, R), kv_rows(m, v, R), m->st);
+  });
+}
+
+// JET_FP32: the sequences of t (all of their tokens as rows) read back into
+// [Hkv][R][hd] buffers of the workspace, R rows in all.
+Status qcache_read_all(jet_model *m, const jetk::QCache &c, const QTables &t, void **k, void **v) {
+  const int64_t R = t.rows.back();
+  const size_t bytes = (size_t)(m->h.n_kv_heads * R * m->h.head_dim) * m->esz;
+  TRY(ws(m, "qc_k", bytes, k));
+  TRY(ws(m, "qc_v", bytes, v));
+  KTimer tm(m, JET_K_OTHER, 0, kv_bytes_of(m, R, (double)m->esz + 1.0));
+  return each_batch(t.b, [&](const jetk::QBatch &b) {
+    return jetk::launch_qcache_read(c, b, kv_rows(m, *k, R), kv_rows(m, *v, R), m->st);
+  });
 }
 
 // Buffers of one forward wave over R rows.
@@ -1077,6 +1174,16 @@ Status palloc(jet_prefix *p, size_t bytes, void **out) {
   return Status::ok();
 }
 
+// K and V buffers of an attention layer (and their scale bytes, in 8 bits).
+Status palloc_kv(jet_model *m, jet_prefix *p, int64_t l, size_t bytes) {
+  TRY(palloc(p, bytes, &p->kcache[(size_t)l]));
+  TRY(palloc(p, bytes, &p->vcache[(size_t)l]));
+  if (m->qfmt < 0) return Status::ok();
+  const size_t eb = (size_t)(m->h.n_kv_heads * (p->qslot0.back() / kQBlock));
+  TRY(palloc(p, eb, (void **)&p->kexp[(size_t)l]));
+  return palloc(p, eb, (void **)&p->vexp[(size_t)l]);
+}
+
 Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *tokens, jet_prefix *p) {
   const ModelHeader &h = m->h;
   TRY(check_offsets(offs, n_q, 1, "prefix_offsets"));
@@ -1089,7 +1196,15 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
   p->n_q = n_q;
   p->prefix_offsets.assign(offs, offs + n_q + 1);
   p->T = T;
-  const size_t kv_bytes = (size_t)(h.n_kv_heads * T * h.head_dim) * m->esz * m->anp;
+  const bool qc = m->qfmt >= 0;
+  if (qc) {
+    p->qslot0.assign(1, 0);
+    for (int32_t q = 0; q < n_q; ++q) p->qslot0.push_back(p->qslot0.back() + q_slots(offs[q + 1] - offs[q]));
+    p->kexp.assign((size_t)h.n_layers, nullptr);
+    p->vexp.assign((size_t)h.n_layers, nullptr);
+  }
+  const size_t kv_bytes = qc ? (size_t)(h.n_kv_heads * p->qslot0.back() * h.head_dim)
+                             : (size_t)(h.n_kv_heads * T * h.head_dim) * m->esz * m->anp;
   p->kcache.assign((size_t)h.n_layers, nullptr);
   p->vcache.assign((size_t)h.n_layers, nullptr);
   p->S_pre.assign((size_t)h.n_layers, nullptr);
@@ -1103,8 +1218,7 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
       HIPC(hipMemsetAsync(p->conv_tail[(size_t)l], 0, tb, m->st));
       continue;
     }
-    TRY(palloc(p, kv_bytes, &p->kcache[(size_t)l]));
-    TRY(palloc(p, kv_bytes, &p->vcache[(size_t)l]));
+    TRY(palloc_kv(m, p, l, kv_bytes));
   }
   TRY(palloc(p, (size_t)(n_q * h.d) * m->esz * m->np, &p->f_last));
 
@@ -1131,10 +1245,26 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
       last[(size_t)(q - q0)] = (int32_t)(offs[q] - t0 + P - 1);
       qd.qrow0.push_back((int32_t)(offs[q] - t0));
       qd.nrows.push_back((int32_t)P);
-      qd.pre_slot0.push_back(offs[q]);
+      qd.pre_slot0.push_back(qc ? offs[q] - t0 : offs[q]);
       qd.pre_len.push_back((int32_t)P);
       qd.suf_row0.push_back(0);
       qd.suf_len.push_back(0);
+    }
+    // caches in 8 bits: the wave's own keys are attended to as they are, in a
+    // cache of the wave's rows, and written to the retained one layer by layer
+    QTables qt;
+    void *wk = nullptr, *wv = nullptr;
+    if (qc) {
+      for (int32_t q = q0; q < q1; ++q) {
+        qt.slot0.push_back(p->qslot0[(size_t)q]);
+        qt.len.push_back((int32_t)(offs[q + 1] - offs[q]));
+        qt.rows.push_back((int32_t)(offs[q] - t0));
+      }
+      qt.rows.push_back((int32_t)R);
+      TRY(upload_batch(m, "pre_qc_", &qt));
+      const size_t wb = (size_t)(h.n_kv_heads * R * h.head_dim) * m->esz;
+      TRY(ws(m, "pre_k", wb, &wk));
+      TRY(ws(m, "pre_v", wb, &wv));
     }
     int32_t *d_pos, *d_last;
     TRY(upload(m, "pre_pos", pos, &d_pos));
@@ -1189,10 +1319,11 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
         TRY(ffn(m, ly, b, R));
         continue;
       }
-      TRY(attn_in(m, ly, b, R, d_pos, p->kcache[(size_t)l], p->vcache[(size_t)l], T, t0));
+      void *kc = qc ? wk : p->kcache[(size_t)l], *vc = qc ? wv : p->vcache[(size_t)l];
+      TRY(attn_in(m, ly, b, R, d_pos, kc, vc, qc ? R : T, qc ? 0 : t0));
+      if (qc) TRY(qcache_write(m, qcache_of(m, p, l), qt, wk, wv, R));
       if (l == L - 1 && last_rows_only) break;
-      TRY(run_attention(m, plan, b.q, R, b.att, p->kcache[(size_t)l], p->vcache[(size_t)l], T, nullptr, nullptr,
-                        0, nullptr, nullptr));
+      TRY(run_attention(m, plan, b.q, R, b.att, kc, vc, qc ? R : T, nullptr, nullptr, 0, nullptr, nullptr));
       TRY(attn_out(m, ly, b, R));
       route_rows_set(m, 0, l, t0, R);
       TRY(ffn(m, ly, b, R));
@@ -1205,7 +1336,7 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
         const int64_t P = offs[q + 1] - offs[q];
         ql.qrow0.push_back(last[(size_t)(q - q0)]);
         ql.nrows.push_back(1);
-        ql.pre_slot0.push_back(offs[q]);
+        ql.pre_slot0.push_back(qc ? offs[q] - t0 : offs[q]);
         ql.pre_len.push_back((int32_t)P);
         ql.suf_row0.push_back(0);
         ql.suf_len.push_back(0);
@@ -1214,8 +1345,8 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
       TRY(plan_attention(m, 1, ql, "pre_lr_", &lp));
       int32_t *d_zero_t;
       TRY(upload(m, "pre_lr_t", zero_t, &d_zero_t));
-      TRY(run_attention(m, lp, b.q, R, b.att, p->kcache[(size_t)(L - 1)], p->vcache[(size_t)(L - 1)], T, nullptr,
-                        nullptr, 0, nullptr, d_zero_t, JET_K_ATTN_PREFIX));
+      TRY(run_attention(m, lp, b.q, R, b.att, qc ? wk : p->kcache[(size_t)(L - 1)], qc ? wv : p->vcache[(size_t)(L - 1)],
+                        qc ? R : T, nullptr, nullptr, 0, nullptr, d_zero_t, JET_K_ATTN_PREFIX));
       WaveBufs c;  // the last rows, compacted
       const size_t pe = (size_t)m->np * m->esz, pa = (size_t)m->anp * m->esz;
       TRY(ws_t<float>(m, "lr_resid", (size_t)(nq * h.d), &c.resid));
@@ -1262,7 +1393,8 @@ Status prefill(jet_model *m, int32_t n_q, const int64_t *offs, const int32_t *to
 // delta-rule layers continue the question's state and convolution tail in
 // place. The caches are laid out again once, with room for the n rows after
 // each question, so the prefix stays a plain prefix of P_q + n tokens.
-Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed, int32_t *out) {
+Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed, const jet_trace_rules *rules,
+                int32_t *out) {
   const ModelHeader &h = m->h;
   if (n < 0) return Status::err(JET_E_INVALID, "n_steps must be >= 0");
   if (!(tau >= 0.0f) || !std::isfinite(tau)) return Status::err(JET_E_INVALID, "temperature must be finite and >= 0");
@@ -1273,8 +1405,9 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   for (int32_t q = 0; q < nq; ++q)
     if (offs[q + 1] - offs[q] + n > m->max_ctx)
       return Status::err(JET_E_CAPACITY, "prefix " + std::to_string(q) + " plus the trace is longer than max_ctx");
+  TRY(check_rules(rules, nq, n, h.vocab));
   if (n == 0) return Status::ok();
-  const bool out_dev = out && is_device_ptr(out);
+  const bool out_dev = out && is_device_ptr(out), qc = m->qfmt >= 0;
   const int64_t T = p->T, T2 = T + (int64_t)nq * n, V = h.vocab;
   std::vector<int64_t> offs2((size_t)nq + 1);
   for (int32_t q = 0; q <= nq; ++q) offs2[(size_t)q] = offs[(size_t)q] + (int64_t)q * n;
@@ -1286,12 +1419,18 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   const int64_t nblk = m->anp * h.n_kv_heads;
   const int64_t row_bytes = h.head_dim * (int64_t)m->esz;
   const int64_t R = nq;
-  std::vector<void *> fresh;  // new K then V cache of each attention layer
+  std::vector<int64_t> qslot2(1, 0);  // 8 bits: questions' slots with room for the trace
+  if (qc)
+    for (int32_t q = 0; q < nq; ++q)
+      qslot2.push_back(qslot2.back() + q_slots(offs[(size_t)q + 1] - offs[(size_t)q] + n));
+  const size_t new_kv = qc ? (size_t)(h.n_kv_heads * qslot2.back() * h.head_dim) : (size_t)(nblk * T2 * row_bytes);
+  const size_t new_exp = (size_t)(h.n_kv_heads * (qslot2.back() / kQBlock));
+  std::vector<void *> fresh;  // new K then V cache of each attention layer (and their scale bytes)
   for (int64_t l = 0; l < h.n_layers; ++l) {
     if (m->layers[(size_t)l].gdn) continue;
-    for (int kv = 0; kv < 2; ++kv) {
+    for (int kv = 0; kv < (qc ? 4 : 2); ++kv) {
       void *nb;
-      TRY(palloc(p, (size_t)(nblk * T2 * row_bytes), &nb));
+      TRY(palloc(p, kv < 2 ? new_kv : new_exp, &nb));
       fresh.push_back(nb);
     }
   }
@@ -1300,21 +1439,124 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   float *logits;
   void *kt, *vt;
   TRY(upload(m, "gen_offs", offs, &d_offs));
-  TRY(ws_t<int32_t>(m, "gen_tok", (size_t)(R * n), &d_tok));
+  // A question's tokens so far: its context for the rules (none without them),
+  // ending at column ctx of its row, then the trace.
+  int64_t ctx = 0;
+  if (rules && rules->context_offsets)
+    for (int32_t q = 0; q < nq; ++q) ctx = std::max(ctx, rules->context_offsets[q + 1] - rules->context_offsets[q]);
+  const int64_t ldt = ctx + n;
+  if (R * ldt > (1 << 30)) return Status::err(JET_E_INVALID, "context and trace tokens exceed 2^30");
+  int32_t *d_hist;
+  TRY(ws_t<int32_t>(m, "gen_tok", (size_t)(R * ldt), &d_hist));
+  d_tok = d_hist + ctx;
   TRY(ws_t<float>(m, "gen_logits", (size_t)(R * V), &logits));
   TRY(ws(m, "gen_k", (size_t)(nblk * R * row_bytes), &kt));
   TRY(ws(m, "gen_v", (size_t)(nblk * R * row_bytes), &vt));
   void *samp;
   TRY(ws(m, "gen_sample", (size_t)jetk::sample_scratch_bytes((int)R), &samp));
   TRY(upload(m, "gen_zero_t", std::vector<int32_t>((size_t)R, 0), &d_zero_t));
+  // the rules' arrays, and the workspace of attention in 8 bits
+  jetk::LogitsArgs la{};
+  int32_t *d_hbeg = nullptr, *d_hend = nullptr;
+  if (rules) {
+    std::vector<int32_t> hist((size_t)(R * ldt), 0), beg((size_t)R), nctx((size_t)R, 0), boff;
+    for (int32_t q = 0; q < nq; ++q) {
+      const int64_t c0 = rules->context_offsets ? rules->context_offsets[q] : 0;
+      const int64_t nc = rules->context_offsets ? rules->context_offsets[q + 1] - c0 : 0;
+      beg[(size_t)q] = (int32_t)(q * ldt + ctx - nc);
+      nctx[(size_t)q] = (int32_t)nc;
+      for (int64_t i = 0; i < nc; ++i) hist[(size_t)(beg[(size_t)q] + i)] = rules->context_tokens[c0 + i];
+    }
+    TRY(upload(m, "gen_tok", hist, &d_hist));
+    int32_t *d_nctx;
+    TRY(upload(m, "gen_hbeg", beg, &d_hbeg));
+    TRY(upload(m, "gen_nctx", nctx, &d_nctx));
+    TRY(ws_t<int32_t>(m, "gen_hend", (size_t)R, &d_hend));
+    float *d_rep, *d_pres, *d_freq;
+    TRY(upload(m, "gen_rep", std::vector<float>((size_t)R, rules->repetition), &d_rep));
+    TRY(upload(m, "gen_pres", std::vector<float>((size_t)R, rules->presence), &d_pres));
+    TRY(upload(m, "gen_freq", std::vector<float>((size_t)R, rules->frequency), &d_freq));
+    la.R = (int)R;
+    la.V = (int)V;
+    la.in = la.out = logits;
+    la.in_ld = la.out_ld = V;
+    la.h_off = d_hbeg;
+    la.h_end = d_hend;
+    la.h_ids = d_hist;
+    la.n_hist = (int)(R * ldt);
+    la.h_prompt = d_nctx;
+    la.rep = d_rep;
+    la.pres = d_pres;
+    la.freq = d_freq;
+    if (rules->bias_offsets) {
+      const int64_t nb = rules->bias_offsets[nq];
+      int32_t *d_boff, *d_bid;
+      float *d_bval;
+      TRY(upload(m, "gen_boff", std::vector<int32_t>(rules->bias_offsets, rules->bias_offsets + nq + 1), &d_boff));
+      TRY(upload(m, "gen_bid", std::vector<int32_t>(rules->bias_tokens, rules->bias_tokens + nb), &d_bid));
+      TRY(upload(m, "gen_bval", std::vector<float>(rules->bias_values, rules->bias_values + nb), &d_bval));
+      la.b_off = d_boff;
+      la.b_ids = d_bid;
+      la.b_val = d_bval;
+      la.n_bias = (int)nb;
+    }
+    if (rules->n_masks > 0) {
+      const int64_t words = (V + 31) / 32;
+      uint32_t *d_masks;
+      TRY(upload(m, "gen_masks", std::vector<uint32_t>(rules->masks, rules->masks + rules->n_masks * words), &d_masks));
+      int32_t *d_mi;
+      TRY(ws_t<int32_t>(m, "gen_mi", (size_t)R, &d_mi));
+      la.masks = d_masks;
+      la.n_masks = rules->n_masks;
+      la.mask_ld = words;
+      la.mask_index = d_mi;
+    }
+  }
+  void *qws = nullptr;
+  int64_t *d_qs_old = nullptr, *d_qs_new = nullptr;
+  int32_t *d_qlen = nullptr;
+  if (qc) {
+    int64_t longest = 0, total = 0;
+    std::vector<int32_t> len((size_t)nq);
+    for (int32_t q = 0; q < nq; ++q) {
+      len[(size_t)q] = (int32_t)(offs[(size_t)q + 1] - offs[(size_t)q]);
+      longest = std::max<int64_t>(longest, len[(size_t)q]);
+      total += len[(size_t)q] + n;
+    }
+    // the most that any step needs (its plan depends on its longest sequence)
+    const jetk::QCache c = qcache_view(m, nullptr, nullptr, nullptr, nullptr, qslot2.back());
+    int64_t need = 0;
+    if (m->kdt != 1 && nq <= kMaxSeqs)
+      for (int32_t t = 1; t <= n; ++t) {
+        const jetk::QBatch b{nq, nq, 1, longest + t, nullptr, nullptr, nullptr};
+        need = std::max(need, jetk::qattn_workspace(c, b, (int)h.n_heads));
+      }
+    if (m->kdt == 1) {  // the caches as read back
+      void *unused;
+      const size_t bytes = (size_t)(h.n_kv_heads * total * h.head_dim) * m->esz;
+      TRY(ws(m, "qc_k", bytes, &unused));
+      TRY(ws(m, "qc_v", bytes, &unused));
+    }
+    TRY(ws(m, "gen_qws", (size_t)need, &qws));
+    TRY(upload(m, "gen_qs_old", p->qslot0, &d_qs_old));
+    TRY(upload(m, "gen_qs_new", qslot2, &d_qs_new));
+    TRY(upload(m, "gen_qlen", len, &d_qlen));
+  }
   // attention caches laid out again with n free rows after each question
   size_t fi = 0;
   for (int64_t l = 0; l < h.n_layers; ++l) {
     if (m->layers[(size_t)l].gdn) continue;
-    for (int kv = 0; kv < 2; ++kv) {
-      void *&buf = kv ? p->vcache[(size_t)l] : p->kcache[(size_t)l];
+    if (qc) {
+      KTimer t(m, JET_K_OTHER, 0, 0);
+      const jetk::QCache to = qcache_view(m, fresh[fi], fresh[fi + 1], (uint8_t *)fresh[fi + 2], (uint8_t *)fresh[fi + 3],
+                                          qslot2.back());
+      LAUNCH(jetk::launch_qcache_copy(qcache_of(m, p, l), to, d_qs_old, d_qs_new, d_qlen, nq, m->st));
+    }
+    for (int kv = 0; kv < (qc ? 4 : 2); ++kv) {
+      void *buf = kv == 0 ? p->kcache[(size_t)l] : kv == 1 ? p->vcache[(size_t)l]
+                : kv == 2 ? (void *)p->kexp[(size_t)l] : (void *)p->vexp[(size_t)l];
       void *nb = fresh[fi++];
-      {
+      if (!qc) {
         KTimer t(m, JET_K_OTHER, 0, 0);
         LAUNCH(jetk::launch_kv_relayout(buf, nb, d_offs, nq, (int)nblk, T, T2, row_bytes, n, m->st));
       }
@@ -1327,30 +1569,55 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
           p->allocs.erase(p->allocs.begin() + (std::ptrdiff_t)i);
           break;
         }
-      buf = nb;
+      if (kv == 0) p->kcache[(size_t)l] = nb;
+      else if (kv == 1) p->vcache[(size_t)l] = nb;
+      else if (kv == 2) p->kexp[(size_t)l] = (uint8_t *)nb;
+      else p->vexp[(size_t)l] = (uint8_t *)nb;
     }
   }
+  if (qc) p->qslot0 = qslot2;
 
   const int64_t gH = h.gdn_heads;
   for (int32_t t = 0; t < n; ++t) {
     // token t of every question from the current last rows
     TRY(run_gemm(m, JET_K_LMHEAD, jetk::EPI_STORE_F32, p->f_last, m->np * h.d, m->pair, m->lm_head, h.d, R, V, h.d,
                  logits, V, m->is_lm));
+    if (rules) {
+      std::vector<int32_t> end((size_t)R), mi((size_t)R, -1);
+      for (int32_t q = 0; q < nq; ++q) {
+        end[(size_t)q] = (int32_t)(q * ldt + ctx + t);
+        if (la.masks) mi[(size_t)q] = rules->mask_index[(int64_t)q * n + t];
+      }
+      TRY(upload(m, "gen_hend", end, &d_hend));
+      int32_t *d_mi;
+      if (la.masks) TRY(upload(m, "gen_mi", mi, &d_mi));
+      KTimer tm(m, JET_K_OTHER, 0, 0);
+      LAUNCH(jetk::launch_logits_adjust(la, m->st));
+    }
     {
       KTimer tm(m, JET_K_OTHER, 0, 0);
-      LAUNCH(jetk::launch_sample(logits, V, (int)R, (int)V, (double)tau, seed, 0, t, samp, d_tok + t, n, m->st));
+      LAUNCH(jetk::launch_sample(logits, V, (int)R, (int)V, (double)tau, seed, 0, t, samp, d_tok + t, ldt, m->st));
     }
     // ... and through the model at positions P_q + t
     std::vector<int32_t> pos((size_t)R), idx((size_t)R), slot((size_t)R);
     QDesc qd;
+    QTables qt, ra;  // 8 bits: the step's row of each sequence, and all of its rows
+    ra.rows.push_back(0);
     for (int32_t q = 0; q < nq; ++q) {
       const int64_t P = offs[(size_t)q + 1] - offs[(size_t)q];
       pos[(size_t)q] = (int32_t)(P + t);
-      idx[(size_t)q] = q * n + t;
+      idx[(size_t)q] = (int32_t)(q * ldt + t);
       slot[(size_t)q] = (int32_t)(offs2[(size_t)q] + P + t);
+      if (qc) {
+        qt.slot0.push_back(qslot2[(size_t)q]);
+        qt.len.push_back((int32_t)(P + t + 1));
+        qt.rows.push_back(q);
+        ra.rows.push_back(ra.rows.back() + (int32_t)(P + t + 1));
+      }
       qd.qrow0.push_back(q);
       qd.nrows.push_back(1);
-      qd.pre_slot0.push_back(offs2[(size_t)q]);
+      // (JET_FP32 in 8 bits: the rows read back lie one question after another)
+      qd.pre_slot0.push_back(qc ? ra.rows[(size_t)q] : offs2[(size_t)q]);
       qd.pre_len.push_back((int32_t)(P + t + 1));
       qd.suf_row0.push_back(0);
       qd.suf_len.push_back(0);
@@ -1361,6 +1628,15 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
     TRY(upload(m, "gen_slot", slot, &d_slot));
     AttnPlan plan;
     TRY(plan_attention(m, 1, qd, "gen_at_", &plan));
+    if (qc) {
+      qt.rows.push_back(nq);
+      TRY(upload_batch(m, "gen_qc_", &qt));
+      if (m->kdt == 1) {
+        ra.slot0 = qt.slot0;
+        ra.len = qt.len;
+        TRY(upload_batch(m, "gen_qa_", &ra));
+      }
+    }
     GdnPlan gp;
     if (h.hybrid) {
       // the convolution tail of question q is a ring of its last 3 input
@@ -1393,6 +1669,25 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
         continue;
       }
       TRY(attn_in(m, ly, b, R, d_pos, kt, vt, R, 0));
+      if (qc) {
+        const jetk::QCache c = qcache_of(m, p, l);
+        TRY(qcache_write(m, c, qt, kt, vt, R));
+        if (m->kdt == 1) {
+          void *ck, *cv;
+          TRY(qcache_read_all(m, c, ra, &ck, &cv));
+          TRY(run_attention(m, plan, b.q, R, b.att, ck, cv, ra.rows.back(), nullptr, nullptr, 0, nullptr, d_zero_t));
+        } else {
+          const int64_t hq = h.n_heads * h.head_dim;
+          KTimer tm(m, JET_K_ATTN_CAND, plan.flops, kv_bytes_of(m, ra.rows.back(), 1.0));
+          TRY(each_batch(qt.b, [&](const jetk::QBatch &qb) {
+            const jetk::QRows q{b.q, 1, 1, hq, h.head_dim}, o{b.att, 1, 1, hq, h.head_dim};
+            return jetk::launch_qattn({c, qb, q, o, (int)h.n_heads, 1, plan.a.scale, nullptr, qws}, m->st);
+          }));
+        }
+        TRY(attn_out(m, ly, b, R));
+        TRY(ffn(m, ly, b, R));
+        continue;
+      }
       {
         KTimer tm(m, JET_K_OTHER, 0, 0);
         LAUNCH(jetk::launch_kv_append(kt, p->kcache[(size_t)l], d_slot, (int)R, (int)nblk, T2, row_bytes, m->st));
@@ -1424,9 +1719,10 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
       HIPC(hipMemcpyAsync(p->conv_tail[(size_t)l], tmp, (size_t)(nq * 3 * gC) * 4, hipMemcpyDeviceToDevice, m->st));
     }
   }
-  std::vector<int32_t> toks((size_t)(R * n));
-  HIPC(hipMemcpyAsync(toks.data(), d_tok, toks.size() * 4, hipMemcpyDeviceToHost, m->st));
+  std::vector<int32_t> all((size_t)(R * ldt)), toks((size_t)(R * n));
+  HIPC(hipMemcpyAsync(all.data(), d_hist, all.size() * 4, hipMemcpyDeviceToHost, m->st));
   TRY(sync(m));
+  for (int64_t q = 0; q < R; ++q) std::copy_n(all.begin() + q * ldt + ctx, n, toks.begin() + q * n);
   for (int32_t v : toks)
     if (v < 0) return Status::err(JET_E_DEVICE, "sampling met no finite logit");
   p->prefix_offsets = offs2;
@@ -1539,6 +1835,15 @@ Status score(jet_model *m, const jet_prefix *p, const int64_t *qco, const int64_
   std::vector<int32_t> cand_q((size_t)N);
   for (int32_t q = 0; q < p->n_q; ++q)
     for (int64_t c = qco[q]; c < qco[q + 1]; ++c) cand_q[(size_t)c] = q;
+  // retained caches in 8 bits: attended to there, or in JET_FP32 read back
+  const bool qown = m->qfmt >= 0 && m->kdt != 1;
+  QTables qt;
+  if (m->qfmt >= 0 && !qown) {
+    qt.slot0.assign(p->qslot0.begin(), p->qslot0.end() - 1);
+    qt.rows.assign(p->prefix_offsets.begin(), p->prefix_offsets.end());
+    for (int32_t q = 0; q < p->n_q; ++q) qt.len.push_back(qt.rows[(size_t)q + 1] - qt.rows[(size_t)q]);
+    TRY(upload_batch(m, "cand_qc_", &qt));
+  }
   auto row0 = [&](int64_t c) { return c < N ? (int64_t)L.cand_row0[(size_t)c] : L.n_rows; };
   route_rows_begin(m, 1, L.n_rows);
 
@@ -1549,6 +1854,8 @@ Status score(jet_model *m, const jet_prefix *p, const int64_t *qco, const int64_
     m->arena_mark = m->arena_top;
     double per_row = 0, fixed = 0;
     wave_bytes_bound(m, &per_row, &fixed);
+    if (m->qfmt >= 0 && !qown)  // the prefixes as read back
+      fixed += 2.0 * (double)(h.n_kv_heads * p->T * h.head_dim) * (double)m->esz;
     const double room = (double)m->arena_cap - (double)m->arena_mark - fixed;
     const int64_t fit = room > per_row ? (int64_t)(room / per_row) : 0;
     int64_t longest = 0;
@@ -1581,14 +1888,15 @@ Status score(jet_model *m, const jet_prefix *p, const int64_t *qco, const int64_
         const int64_t a = row0(c) - r0, e = row0(ce) - r0;
         qd.qrow0.push_back((int32_t)a);
         qd.nrows.push_back((int32_t)(e - a));
-        qd.pre_slot0.push_back(p->prefix_offsets[(size_t)q]);
+        // (caches in 8 bits: its slots there, or in JET_FP32 its rows as read back)
+        qd.pre_slot0.push_back(qown ? p->qslot0[(size_t)q] : p->prefix_offsets[(size_t)q]);
         qd.pre_len.push_back((int32_t)(p->prefix_offsets[(size_t)q + 1] - p->prefix_offsets[(size_t)q]));
         qd.suf_row0.push_back((int32_t)a);
         qd.suf_len.push_back((int32_t)(e - a));
         c = ce;
       }
       AttnPlan plan;
-      TRY(plan_attention(m, 1, qd, "cand_at_", &plan));
+      TRY(plan_attention(m, 1, qd, "cand_at_", &plan, qown));
       GdnPlan gp;
       if (h.hybrid) {
         // conv history: own earlier rows, then the question's prefix tail
@@ -1624,8 +1932,22 @@ Status score(jet_model *m, const jet_prefix *p, const int64_t *qco, const int64_
           TRY(gdn_layer(m, ly, b, R, gp, p->conv_tail[(size_t)l], p->S_pre[(size_t)l], nullptr));
         } else {
           TRY(attn_in(m, ly, b, R, d_rpos + r0, kc, vc, R, 0));
-          TRY(run_attention(m, plan, b.q, R, b.att, p->kcache[(size_t)l], p->vcache[(size_t)l], p->T, kc, vc, R,
-                            d_rc + r0, d_rt + r0));
+          if (qown) {
+            const int64_t hq = h.n_heads * h.head_dim;
+            jetk::QAttn a{};
+            a.c = qcache_of(m, p, l);
+            a.q = {b.q, 1, 1, hq, h.head_dim};
+            a.out = {b.att, 1, 1, hq, h.head_dim};
+            a.Hq = (int)h.n_heads;
+            a.scale = plan.a.scale;
+            KTimer t(m, JET_K_ATTN_CAND, plan.flops, plan.bytes);
+            LAUNCH(jetk::launch_qattn_own(
+                a, {plan.a.items, plan.a.qs, kc, vc, R, d_rc + r0, d_rt + r0, plan.a.n_items}, m->st));
+          } else {
+            void *pk = p->kcache[(size_t)l], *pv = p->vcache[(size_t)l];
+            if (m->qfmt >= 0) TRY(qcache_read_all(m, qcache_of(m, p, l), qt, &pk, &pv));
+            TRY(run_attention(m, plan, b.q, R, b.att, pk, pv, p->T, kc, vc, R, d_rc + r0, d_rt + r0));
+          }
           TRY(attn_out(m, ly, b, R));
         }
         route_rows_set(m, 1, l, r0, R);
@@ -1682,6 +2004,8 @@ void free_model(jet_model *m) {
     p->allocs.clear();
     p->kcache.clear();
     p->vcache.clear();
+    p->kexp.clear();
+    p->vexp.clear();
     p->S_pre.clear();
     p->conv_tail.clear();
     p->f_last = nullptr;
@@ -1761,19 +2085,33 @@ extern "C" int jet_prefill_prefix(jet_model *model, int32_t n_q, const int64_t *
   return JET_OK;
 }
 
-extern "C" int jet_generate_trace(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature,
-                                  uint64_t seed, int32_t *out_tokens) {
+static int generate_entry(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature, uint64_t seed,
+                          const jet_trace_rules *rules, int32_t *out_tokens) {
   clear_error();
   if (!model || !prefix) return fail(Status::err(JET_E_INVALID, "model or prefix is NULL"));
   if (prefix->m != model) return fail(Status::err(JET_E_INVALID, "prefix was not made from this model"));
   if (hipSetDevice(model->device) != hipSuccess) return fail(Status::err(JET_E_DEVICE, "hipSetDevice failed"));
-  Status s = generate(model, prefix, n_steps, temperature, seed, out_tokens);
+  Status s = generate(model, prefix, n_steps, temperature, seed, rules, out_tokens);
   if (!s) {
     (void)hipStreamSynchronize(model->st);
     drain_timers(model);
     return fail(s);
   }
   return JET_OK;
+}
+
+extern "C" int jet_generate_trace(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature,
+                                  uint64_t seed, int32_t *out_tokens) {
+  return generate_entry(model, prefix, n_steps, temperature, seed, nullptr, out_tokens);
+}
+
+extern "C" int jet_generate_trace_rules(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature,
+                                        uint64_t seed, const jet_trace_rules *rules, int32_t *out_tokens) {
+  try {
+    return generate_entry(model, prefix, n_steps, temperature, seed, rules, out_tokens);
+  } catch (const std::exception &) {
+    return fail(Status::err(JET_E_OOM, "out of host memory"));
+  }
 }
 
 extern "C" int jet_score_candidates(jet_model *model, const jet_prefix *prefix, const int64_t *q_cand_offsets,

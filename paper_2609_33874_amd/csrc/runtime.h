@@ -71,6 +71,7 @@ struct jet_model {
   hipStream_t st = nullptr;
   int64_t max_ctx = 0, prefill_budget = 0, wave_budget = 0, max_bytes = 0;
   int flags = 0;
+  int qfmt = -1;   // 8-bit format of retained attention caches, or -1 (JET_FLAG_QCACHE_*)
   size_t esz = 2;  // bytes per compute element
   size_t bytes_used = 0;
   void *embed = nullptr, *lm_head = nullptr;
@@ -114,6 +115,10 @@ struct jet_prefix {
   std::vector<int64_t> prefix_offsets;
   int64_t T = 0;                     // total prefix tokens
   std::vector<void *> kcache, vcache;  // per layer (attention layers only), [planes][Hkv][T][hd]
+  // JET_FLAG_QCACHE_*: kcache / vcache hold bytes [Hkv][S][hd], kexp / vexp their
+  // scale bytes [Hkv][S / 32], question q from slot qslot0[q] (S: n_q + 1st)
+  std::vector<uint8_t *> kexp, vexp;
+  std::vector<int64_t> qslot0;
   std::vector<float *> S_pre;        // per layer (delta-rule only), [n_q][H][dv][dk]
   std::vector<float *> conv_tail;    // per layer (delta-rule only), [n_q][kc-1][C]
   void *f_last = nullptr;            // [n_q][planes * d] final-normed last prefix rows

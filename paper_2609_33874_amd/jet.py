@@ -20,6 +20,7 @@ JET_BF16, JET_FP32, JET_BF16_SINGLE, JET_F16, JET_F16P = 0, 1, 2, 3, 4
 JET_CHOICE, JET_BINARY, JET_ORDINAL = 0, 1, 2
 JET_FLAG_KERNEL_TIMING = 1
 JET_FLAG_RECORD_ROUTES = 2
+JET_FLAG_QCACHE_INT8, JET_FLAG_QCACHE_E4M3 = 4, 8
 JET_NOALLOC_SCRATCH_BYTES = 64 << 20
 JET_T_F32, JET_T_F16, JET_T_BF16 = 0, 1, 2
 JET_QCACHE_INT8, JET_QCACHE_E4M3 = 0, 1
@@ -33,7 +34,7 @@ EXPORTS = ["jet_model_load", "jet_prefill_prefix", "jet_generate_trace", "jet_sc
            "jet_answer_classes", "jet_evaluate", "jet_candidate_layout", "jet_stats_get", "jet_stats_reset", "jet_model_info",
            "jet_routes_get", "jet_prefix_free", "jet_model_free", "jet_last_error",
            "jet_qcache_write", "jet_qcache_read", "jet_qcache_attention", "jet_qcache_attention_workspace",
-           "jet_logits_adjust"]
+           "jet_logits_adjust", "jet_generate_trace_rules"]
 
 
 class JetError(RuntimeError):
@@ -56,6 +57,13 @@ class jet_stats(ctypes.Structure):
                 ("score_waves", ctypes.c_int64), ("kernel_launches", ctypes.c_int64 * 9),
                 ("kernel_ms", ctypes.c_double * 9), ("kernel_flops", ctypes.c_double * 9),
                 ("kernel_bytes", ctypes.c_double * 9)]
+
+
+class jet_trace_rules(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_float), ("presence", ctypes.c_float), ("frequency", ctypes.c_float),
+                ("n_masks", ctypes.c_int32), ("context_offsets", ctypes.c_void_p), ("context_tokens", ctypes.c_void_p),
+                ("bias_offsets", ctypes.c_void_p), ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("masks", ctypes.c_void_p), ("mask_index", ctypes.c_void_p)]
 
 
 class jet_qcache(ctypes.Structure):
@@ -107,6 +115,8 @@ def lib() -> ctypes.CDLL:
         L.jet_model_load.argtypes = [ctypes.c_char_p, ctypes.POINTER(jet_load_opts), ctypes.POINTER(P)]
         L.jet_prefill_prefix.argtypes = [P, I32, P, P, ctypes.POINTER(P)]
         L.jet_generate_trace.argtypes = [P, P, I32, ctypes.c_float, ctypes.c_uint64, P]
+        L.jet_generate_trace_rules.argtypes = [P, P, I32, ctypes.c_float, ctypes.c_uint64,
+                                               ctypes.POINTER(jet_trace_rules), P]
         L.jet_score_candidates.argtypes = [P, P, P, P, P, P, P]
         L.jet_score_candidates_noalloc.argtypes = [P, P, P, P, P, P, P]
         L.jet_decide.argtypes = [I32, I32, P, P, P, P, P]
@@ -189,6 +199,49 @@ def jet_generate_trace(model, prefix, n_q: int, n_steps: int, temperature: float
         raise TypeError("out must be a contiguous int32 array")
     _check(lib().jet_generate_trace(model, prefix, int(n_steps), float(temperature),
                                     ctypes.c_uint64(seed & 0xFFFFFFFFFFFFFFFF), ot))
+    return out
+
+
+def jet_generate_trace_rules(model, prefix, n_q: int, n_steps: int, temperature: float = 0.0, seed: int = 0, out=None,
+                             repetition: float = 1.0, presence: float = 0.0, frequency: float = 0.0, context=None,
+                             bias=None, masks=None, mask_index=None):
+    """jet_generate_trace with rules for its tokens. context: (offsets [n_q + 1],
+    tokens) that count as seen for `repetition`; bias: (offsets [n_q + 1],
+    tokens, values); masks: uint32 [n_masks, ceil(vocab / 32)], bit v % 32 of
+    word v / 32 allows token v, with mask_index [n_q, n_steps], < 0 for none."""
+    if out is None:
+        out = np.empty((n_q, max(int(n_steps), 0)), np.int32)
+    ot, keep = _ptr(out, np.int32)
+    if isinstance(out, np.ndarray) and keep is not out:
+        raise TypeError("out must be a contiguous int32 array")
+    r = jet_trace_rules(repetition, presence, frequency, 0)
+    held = []
+
+    def host(x, dtype, size):
+        a = np.ascontiguousarray(x, dtype=dtype)
+        if a.size != size:
+            raise ValueError(f"a rule's array has {a.size} elements instead of {size}")
+        held.append(a)
+        return a.ctypes.data if a.size else None
+
+    if context is not None:
+        off = np.ascontiguousarray(context[0], np.int64)
+        r.context_offsets = host(off, np.int64, n_q + 1)
+        r.context_tokens = host(context[1], np.int32, int(off[-1]))
+    if bias is not None:
+        off = np.ascontiguousarray(bias[0], np.int64)
+        r.bias_offsets = host(off, np.int64, n_q + 1)
+        r.bias_tokens = host(bias[1], np.int32, int(off[-1]))
+        r.bias_values = host(bias[2], np.float32, int(off[-1]))
+    if masks is not None:
+        masks = np.ascontiguousarray(masks, np.uint32)
+        words = (jet_model_info(model)["vocab"] + 31) // 32
+        r.n_masks = masks.shape[0]
+        r.masks = host(masks, np.uint32, r.n_masks * words)
+        if mask_index is not None:
+            r.mask_index = host(mask_index, np.int32, n_q * max(int(n_steps), 0))
+    _check(lib().jet_generate_trace_rules(model, prefix, int(n_steps), float(temperature),
+                                          ctypes.c_uint64(seed & 0xFFFFFFFFFFFFFFFF), ctypes.byref(r), ot))
     return out
 
 
