@@ -48,7 +48,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // those same keys: a transposition of bytes inside the lane makes the A
 // operand, dim HD/16 c + i in product i.
 template <typename T, typename O, int FMT, int HD, int QB>
-__global__ __launch_bounds__(64 * kWaves, HD == 256 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit) {
+__global__ __launch_bounds__(64 * kWaves, HD == 256 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit, int per) {
   constexpr int ND = HD / 16, NK = HD / 32, LD = HD + 4;
   typedef QTile<HD> Tile;
   __shared__ float s_o[kWaves][16 * QB][LD];
@@ -66,9 +66,10 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 ? 2 : 4) void qattn_split_ke
     // keys of this block: up to the last one that its last row sees
     const int last_row = (min(sb + 16 * QB, slots) - 1) / G;
     const int kend = max(0, a.causal ? sq.pos0 + last_row + 1 : sq.len);
-    const int ntile = (kend + kTile - 1) / kTile, per = (ntile + nsplit - 1) / nsplit;
-    const int t1 = min(ntile, (sp + 1) * per);
-    int t = sp * per + wave;
+    const int ntile = (kend + kTile - 1) / kTile;
+    const int t0 = (int)min((int64_t)sp * per, (int64_t)ntile);
+    const int t1 = sp == nsplit - 1 ? ntile : (int)min((int64_t)(sp + 1) * per, (int64_t)ntile);
+    int t = t0 + wave;
 
     // (a tile's rows lie one after another; past the sequence's end its last
     // row's bytes are loaded: those keys are masked)
@@ -339,45 +340,49 @@ __global__ __launch_bounds__(64 * W * NH) void qattn_join_kernel(QAttn a, int ns
 
 // The kernel and the splits of a launch. Query slots of a sequence and KV head
 // (rows * heads of its group) up to kFewSlots take the kernel above, more take
-// the one of k_qattn_rows.hip. Either needs about 512 workgroups, two on each
-// of 256 CUs.
-// Few slots: so many splits that there are 512 workgroups, of 512 keys at least
-// (two tiles a wave) and none up to 1024 keys, where the joining costs more: one
-// question's 731 keys 13.1 us with two splits, 10.9 with one. Twice as many
-// where that leaves 8192 keys each, so that sequences of different lengths do
-// not leave the GPU half empty at the end: 16 of 65536 .. 131072 keys 626 us with
-// 512 workgroups, 583 with 1024; but 64 of 1024 .. 4096 keys 76 and 82 (joining).
-// Many slots: the splits that take the fewest rounds of 512 workgroups over the
-// keys of one, each workgroup counted as 512 keys longer than it is (its
-// queries, its results and their joining): 320 workgroups of 4096 .. 8192 keys
-// take 289 us in 2 splits (640: two rounds, the second nearly empty), 220 in 3.
-constexpr int64_t kFewSlots = 32;
+// the one of k_qattn_rows.hip. Either wants about 512 workgroups, two on each of
+// 256 CUs.
+// Few slots: a split is so many keys of any sequence, so that workgroups are
+// alike and a short sequence has fewer of them (3 sequences of 60000 .. 131072
+// keys: 63 us, 70 with each sequence in 43 equal parts). 512 keys at least, two
+// tiles a wave, and no split up to 1024 keys, where the joining costs more (one
+// question's 731 keys 13.1 us with two splits, 10.9 with one). No more than 6144
+// keys, or the longest sequences end alone: 16 of 65536 .. 131072 keys 633 us in 4
+// splits, 584 in 16, 569 in 24; but 64 of 1024 .. 4096 keys 73 us in one, 81 in
+// four.
+// Many slots: a row's keys in equal parts, so many that they take the fewest
+// rounds of 512 workgroups over the keys of one, each workgroup counted as 512
+// keys longer than it is (its queries, its results and their joining): 320
+// workgroups of 4096 .. 8192 keys take 289 us in 2 splits (640: two rounds, the
+// second nearly empty), 220 in 3.
+constexpr int64_t kFewSlots = 32, kLeastKeys = 512, kMostKeys = 6144, kFill = 512;
 struct Plan {
   bool few;
   int nsplit;
+  int64_t keys;  // of a split (few slots)
 };
 static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
   const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::max<int64_t>(b.max_len, 1);
   const bool few = slots <= kFewSlots;
-  const int64_t block = few ? 16 : qattn_rows_block(c.hd), fill = 512, least = 512;
+  const int64_t block = few ? 16 : qattn_rows_block(c.hd);
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
-  const int64_t most = std::min<int64_t>((len + least - 1) / least, kMaxSplit);
+  const int64_t most = std::min<int64_t>((len + kLeastKeys - 1) / kLeastKeys, kMaxSplit);
   if (few) {
-    if (len <= 2 * least) return {few, 1};
-    int64_t n = std::min<int64_t>(most, (fill + units - 1) / units);
-    if (len / n >= 8192) n = std::min<int64_t>(most, (2 * fill + units - 1) / units);
-    return {few, (int)n};
+    int64_t n = 1;
+    if (len > 2 * kLeastKeys)
+      n = std::min(most, std::max((kFill + units - 1) / units, (len + kMostKeys - 1) / kMostKeys));
+    const int64_t step = kTile * kWaves, keys = ((len + n - 1) / n + step - 1) / step * step;
+    return {few, (int)((len + keys - 1) / keys), keys};
   }
-  Plan p = {few, 1};
-  int64_t best = INT64_MAX;
+  int64_t best = INT64_MAX, at = 1;
   for (int64_t n = 1; n <= most; ++n) {
-    const int64_t cost = (units * n + fill - 1) / fill * ((len + n - 1) / n + least);
+    const int64_t cost = (units * n + kFill - 1) / kFill * ((len + n - 1) / n + kLeastKeys);
     if (cost < best) {
       best = cost;
-      p.nsplit = (int)n;
+      at = n;
     }
   }
-  return p;
+  return {few, (int)at, 0};
 }
 
 int64_t qattn_workspace(const QCache &c, const QBatch &b, int Hq) {
@@ -398,16 +403,16 @@ template <typename O, int HD> static hipError_t run_join(const QAttn &a, int nsp
 }
 
 template <typename T, typename O, int FMT, int HD>
-static hipError_t run_few(const QAttn &a, int nsplit, hipStream_t st) {
+static hipError_t run_few(const QAttn &a, const Plan &p, hipStream_t st) {
   const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H);
-  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)((slots + 15) / 16 * nsplit), a.c.H, a.b.n_seq),
-                     dim3(64 * kWaves), 0, st, a, nsplit);
+  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)((slots + 15) / 16 * p.nsplit), a.c.H, a.b.n_seq),
+                     dim3(64 * kWaves), 0, st, a, p.nsplit, (int)(p.keys / kTile));
   return hipGetLastError();
 }
 
 template <typename T, typename O, int FMT, int HD> static hipError_t run_hd(const QAttn &a, hipStream_t st) {
   const Plan p = plan_of(a.c, a.b, a.Hq);
-  const hipError_t e = p.few ? run_few<T, O, FMT, HD>(a, p.nsplit, st) : launch_qattn_rows(a, p.nsplit, st);
+  const hipError_t e = p.few ? run_few<T, O, FMT, HD>(a, p, st) : launch_qattn_rows(a, p.nsplit, st);
   return e != hipSuccess || p.nsplit == 1 ? e : run_join<O, HD>(a, p.nsplit, st);
 }
 template <typename T, typename O, int FMT> static hipError_t run_fmt(const QAttn &a, hipStream_t st) {

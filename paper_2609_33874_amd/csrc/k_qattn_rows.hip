@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
       const int tid = here(threadIdx.x), lane = tid & 63, g = lane >> 4, l16 = lane & 15;
       const int r_last = (min(sb + BLOCK, slots) - 1) / G;  // last row of the block, in the sequence
       const int kend = OWN || !a.causal ? len : max(0, pos0 + r_last + 1);
-      const int ntile = (kend + KT - 1) / KT, tps = (ntile + nsplit - 1) / nsplit;
+      const int tps = ((kend + KT - 1) / KT + nsplit - 1) / nsplit;
       const int key0 = sp * tps * KT, key1 = min(kend, (sp + 1) * tps * KT);
 
       // The stream of key tiles: the cache's (cs < 0), then for every candidate

@@ -95,8 +95,8 @@ __device__ __forceinline__ float v_scale(int e, int M) {
 }
 __device__ __forceinline__ int v_top(int e) { return e == kExpNaN ? 0 : e; }
 
-// The kernel of k_qattn_rows.hip on a batch (needs no workspace when nsplit is
-// 1).
+// The kernel of k_qattn_rows.hip on a batch, a row's keys in nsplit equal parts
+// (no workspace where nsplit is 1).
 hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st);
 
 }  // namespace jetk

@@ -16,12 +16,15 @@ struct QSeq {
   int64_t slot0;
   int len, n, row0, pos0, lo, hi;
 };
+// s is the same for every lane, and so is what belongs to it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ QSeq qseq(const QBatch &b, const QCache &c, int s) {
   QSeq q;
-  q.slot0 = b.slot0[s];
-  q.len = b.len[s];
-  q.row0 = b.rows ? b.rows[s] : s;
-  const int end = b.rows ? b.rows[s + 1] : s + 1;
+  const int64_t slot0 = b.slot0[s];
+  q.slot0 = (int64_t)((uint64_t)(uint32_t)uniform((int)(slot0 >> 32)) << 32 | (uint32_t)uniform((int)slot0));
+  q.len = uniform(b.len[s]);
+  q.row0 = uniform(b.rows ? b.rows[s] : s);
+  const int end = uniform(b.rows ? b.rows[s + 1] : s + 1);
   q.n = end - q.row0;
   q.lo = q.hi = 0;
   const bool ok = q.slot0 >= 0 && q.slot0 < c.S && (q.slot0 & ((1 << c.lb) - 1)) == 0 && q.row0 >= 0 && end >= q.row0 &&
