@@ -48,7 +48,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // those same keys: a transposition of bytes inside the lane makes the A
 // operand, dim HD/16 c + i in product i.
 template <typename T, typename O, int FMT, int HD, int QB>
-__global__ __launch_bounds__(64 * kWaves, HD == 256 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit, int per) {
+__global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit, int per) {
   constexpr int ND = HD / 16, NK = HD / 32, LD = HD + 4;
   typedef QTile<HD> Tile;
   __shared__ float s_o[kWaves][16 * QB][LD];
@@ -361,10 +361,13 @@ struct Plan {
   int nsplit;
   int64_t keys;  // of a split (few slots)
 };
+// Query slots of a workgroup: 32 where a sequence has more than 16 (head_dim 256
+// has no registers for them, and reads its keys again).
+static int few_block(int hd, int64_t slots) { return slots > 16 && hd < 256 ? 32 : 16; }
 static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
   const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::max<int64_t>(b.max_len, 1);
   const bool few = slots <= kFewSlots;
-  const int64_t block = few ? 16 : qattn_rows_block(c.hd);
+  const int64_t block = few ? few_block(c.hd, slots) : qattn_rows_block(c.hd, slots);
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
   const int64_t most = std::min<int64_t>((len + kLeastKeys - 1) / kLeastKeys, kMaxSplit);
   if (few) {
@@ -402,12 +405,20 @@ template <typename O, int HD> static hipError_t run_join(const QAttn &a, int nsp
   return hipGetLastError();
 }
 
-template <typename T, typename O, int FMT, int HD>
-static hipError_t run_few(const QAttn &a, const Plan &p, hipStream_t st) {
-  const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H);
-  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, 1>), dim3((unsigned)((slots + 15) / 16 * p.nsplit), a.c.H, a.b.n_seq),
+template <typename T, typename O, int FMT, int HD, int QB>
+static hipError_t run_few_qb(const QAttn &a, const Plan &p, hipStream_t st) {
+  const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H), blocks = (slots + 16 * QB - 1) / (16 * QB);
+  hipLaunchKernelGGL((qattn_split_kernel<T, O, FMT, HD, QB>), dim3((unsigned)(blocks * p.nsplit), a.c.H, a.b.n_seq),
                      dim3(64 * kWaves), 0, st, a, p.nsplit, (int)(p.keys / kTile));
   return hipGetLastError();
+}
+template <typename T, typename O, int FMT, int HD>
+static hipError_t run_few(const QAttn &a, const Plan &p, hipStream_t st) {
+  if constexpr (HD < 256) {
+    if (few_block(HD, (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H)) == 32)
+      return run_few_qb<T, O, FMT, HD, 2>(a, p, st);
+  }
+  return run_few_qb<T, O, FMT, HD, 1>(a, p, st);
 }
 
 template <typename T, typename O, int FMT, int HD> static hipError_t run_hd(const QAttn &a, hipStream_t st) {

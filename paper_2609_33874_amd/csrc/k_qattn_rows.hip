@@ -464,8 +464,11 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
   }
 }
 
-// Query slots of a workgroup: 128, or 64 of head_dim 256 (registers).
-int qattn_rows_block(int hd) { return hd == 256 ? 64 : 128; }
+// Query slots of a workgroup: 128, or 64 where no sequence has more (all four
+// waves have queries then: 8 KV heads, 16 sequences of 64 slots and 8192 keys, 113 us and
+// 91)
+// and of head_dim 256 (registers).
+int qattn_rows_block(int hd, int64_t slots) { return hd == 256 || slots <= 64 ? 64 : 128; }
 
 template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
 static hipError_t run_rows(const QAttn &a, const OwnRows &own, int nsplit, hipStream_t st) {
@@ -485,8 +488,12 @@ static hipError_t run_rows(const QAttn &a, const OwnRows &own, int nsplit, hipSt
 
 template <typename T, typename O, int FMT>
 static hipError_t rows_hd(const QAttn &a, int nsplit, hipStream_t st) {
-  if (a.c.hd == 64) return run_rows<T, O, FMT, 64, 2, false>(a, {}, nsplit, st);
-  if (a.c.hd == 128) return run_rows<T, O, FMT, 128, 2, false>(a, {}, nsplit, st);
+  const bool half = qattn_rows_block(a.c.hd, (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H)) == 64;
+  if (a.c.hd == 64)
+    return half ? run_rows<T, O, FMT, 64, 1, false>(a, {}, nsplit, st) : run_rows<T, O, FMT, 64, 2, false>(a, {}, nsplit, st);
+  if (a.c.hd == 128)
+    return half ? run_rows<T, O, FMT, 128, 1, false>(a, {}, nsplit, st)
+                : run_rows<T, O, FMT, 128, 2, false>(a, {}, nsplit, st);
   return run_rows<T, O, FMT, 256, 1, false>(a, {}, nsplit, st);
 }
 template <typename T, typename O> static hipError_t rows_fmt(const QAttn &a, int nsplit, hipStream_t st) {
@@ -498,13 +505,17 @@ hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st) {
   return a.out.type == 0 ? rows_fmt<bf16, float>(a, nsplit, st) : rows_fmt<bf16, bf16>(a, nsplit, st);
 }
 
+template <int FMT, int HD> static hipError_t run_own(const QAttn &a, const OwnRows &own, hipStream_t st) {
+  if (own.block == 64) return run_rows<f16, f16, FMT, HD, 1, true>(a, own, 1, st);
+  if (own.block == 128) return run_rows<f16, f16, FMT, HD, 2, true>(a, own, 1, st);
+  return hipErrorInvalidValue;
+}
+
 hipError_t launch_qattn_own(const QAttn &a, const OwnRows &own, hipStream_t st) {
   if (own.n_items <= 0) return hipSuccess;
   if (a.q.type != 1 || a.out.type != 1) return hipErrorInvalidValue;
-  if (a.c.hd == 64)
-    return a.c.fmt == 0 ? run_rows<f16, f16, 0, 64, 2, true>(a, own, 1, st) : run_rows<f16, f16, 1, 64, 2, true>(a, own, 1, st);
-  if (a.c.hd == 128)
-    return a.c.fmt == 0 ? run_rows<f16, f16, 0, 128, 2, true>(a, own, 1, st) : run_rows<f16, f16, 1, 128, 2, true>(a, own, 1, st);
+  if (a.c.hd == 64) return a.c.fmt == 0 ? run_own<0, 64>(a, own, st) : run_own<1, 64>(a, own, st);
+  if (a.c.hd == 128) return a.c.fmt == 0 ? run_own<0, 128>(a, own, st) : run_own<1, 128>(a, own, st);
   return hipErrorInvalidValue;
 }
 

@@ -298,14 +298,15 @@ hipError_t launch_qattn(const QAttn &a, hipStream_t st);
 // the cache (a.c; a.q, a.out, a.Hq and a.scale as above, a.b unused) and the
 // body rows of their own candidate, as AttnArgs of mode 1 describes them.
 struct OwnRows {
-  const AttnItem *items;  // of at most qattn_rows_block(hd) query slots
+  const AttnItem *items;  // of at most `block` query slots
   AttnQuestions qs;
   const void *K, *V;      // f16 [H][s_suf][hd]
   int64_t s_suf;
   const int32_t *row_n, *row_t;
-  int n_items;
+  int n_items, block;     // block: from qattn_rows_block
 };
-int qattn_rows_block(int hd);
+// Query slots of a workgroup where no sequence has more than `slots`.
+int qattn_rows_block(int hd, int64_t slots);
 hipError_t launch_qattn_own(const QAttn &a, const OwnRows &own, hipStream_t st);
 // Sequences' blocks [0, len) from one cache into another of the same form:
 // slot0 in either (device, [n_seq]).

@@ -714,10 +714,11 @@ Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, 
   std::vector<jetk::AttnItem> items;
   double pairs = 0;
   double slots = 0, nq = 0;
+  int64_t widest = 0;
   for (auto n : qd.nrows)
-    if (n > 0) slots += (double)G * n, nq += 1;
+    if (n > 0) slots += (double)G * n, nq += 1, widest = std::max(widest, (int64_t)G * n);
   const int block = own_cache
-                        ? jetk::qattn_rows_block((int)h.head_dim)
+                        ? jetk::qattn_rows_block((int)h.head_dim, widest)
                         : jetk::attn_block(m->kdt, m->apair, mode, nq > 0 ? slots / nq : 0, slots * (double)h.n_kv_heads);
   build_items(qd, G, (int)h.n_kv_heads, mode == 0, block, &items, &pairs);
   // Longest work first: the dispatcher hands out workgroups in order, so long
@@ -1942,7 +1943,8 @@ Status score(jet_model *m, const jet_prefix *p, const int64_t *qco, const int64_
             a.scale = plan.a.scale;
             KTimer t(m, JET_K_ATTN_CAND, plan.flops, plan.bytes);
             LAUNCH(jetk::launch_qattn_own(
-                a, {plan.a.items, plan.a.qs, kc, vc, R, d_rc + r0, d_rt + r0, plan.a.n_items}, m->st));
+                a, {plan.a.items, plan.a.qs, kc, vc, R, d_rc + r0, d_rt + r0, plan.a.n_items, plan.a.block},
+                m->st));
           } else {
             void *pk = p->kcache[(size_t)l], *pv = p->vcache[(size_t)l];
             if (m->qfmt >= 0) TRY(qcache_read_all(m, qcache_of(m, p, l), qt, &pk, &pv));
