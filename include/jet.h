@@ -441,7 +441,8 @@ enum { JET_T_F32 = 0, JET_T_F16 = 1, JET_T_BF16 = 2 };
  * less than one step in all, however often it grows.
  *   JET_QCACHE_INT8: value = q 2^e, q = -127 .. 127. e is the least, and not
  *     under -60, with max|x| <= 127 2^e; q = x 2^-e rounded to nearest even.
- *   JET_QCACHE_E4M3: value = f 2^e, f an OCP e4m3 number; max|x| <= 448 2^e. */
+ *   JET_QCACHE_E4M3: value = f 2^e, f an OCP e4m3 number (its NaN bytes 0x7f
+ *     and 0xff are never written, nor expected); max|x| <= 448 2^e. */
 enum { JET_QCACHE_INT8 = 0, JET_QCACHE_E4M3 = 1 };
 
 /* A cache: K and V of n_heads KV heads over n_slots token slots. */
@@ -471,7 +472,7 @@ typedef struct {
                          Larger values in row_offsets and len are still worked
                          off, only slower. */
   const int64_t *slot0;       /* device, [n_seq] */
-  const int32_t *len;         /* device, [n_seq] */
+  const int32_t *len;         /* device, [n_seq], 0 .. 2^30 */
   const int32_t *row_offsets; /* device, [n_seq + 1], or NULL: row s is the one
                                  row of sequence s (n_rows >= n_seq) */
 } jet_qcache_batch;
@@ -513,12 +514,13 @@ int jet_qcache_read(const jet_qcache *cache, const jet_qcache_batch *batch, cons
  * jet_qcache_attention - attention of the batch's rows over the cache (which
  * holds the rows' own tokens already).
  *   n_q_heads: a multiple of cache->n_heads; query head h reads KV head
- *     h / (n_q_heads / cache->n_heads). At most 64 query heads a KV head.
+ *     h / (n_q_heads / cache->n_heads). At most 64 query heads a KV head and
+ *     32768 in all; n_rows times the heads of a KV head at most 2^30.
  *   scale: finite; scores are scale * q . k.
  *   causal: 1: a row sees the tokens up to its own; 0: it sees all len[s].
  *   q: rows of n_q_heads heads, JET_T_F16 or JET_T_BF16.
- *   out: rows of n_q_heads heads, of q's type or JET_T_F32. A row that sees no
- *     token gets zeros. Rows of no sequence are left as they were.
+ *   out: rows of n_q_heads heads, of q's type or JET_T_F32, apart from q's. A
+ *     row that sees no token gets zeros. Rows of no sequence are left as they were.
  *   lse: device, float[n_rows * n_q_heads] or NULL: ln of the sum of e^score
  *     of each (row, head); -inf for a row that sees no token.
  *   workspace: device, 16-byte aligned, at least the bytes that

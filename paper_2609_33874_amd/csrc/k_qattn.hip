@@ -365,7 +365,7 @@ struct Plan {
 // has no registers for them, and reads its keys again).
 static int few_block(int hd, int64_t slots) { return slots > 16 && hd < 256 ? 32 : 16; }
 static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
-  const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::max<int64_t>(b.max_len, 1);
+  const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::min(std::max<int64_t>(b.max_len, 1), (int64_t)1 << 30);
   const bool few = slots <= kFewSlots;
   const int64_t block = few ? few_block(c.hd, slots) : qattn_rows_block(c.hd, slots);
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);

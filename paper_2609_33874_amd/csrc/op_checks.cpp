@@ -62,6 +62,7 @@ Status check_q_heads(const jet_qcache *c, int32_t n_q_heads, float scale) {
   if (!std::isfinite(scale)) return bad("scale must be finite");
   if (n_q_heads < 1 || n_q_heads % c->n_heads) return bad("n_q_heads must be a multiple of the cache's heads");
   if (n_q_heads / c->n_heads > 64) return bad("at most 64 query heads a KV head");
+  if (n_q_heads > 32768) return bad("at most 32768 query heads");
   return Status::ok();
 }
 

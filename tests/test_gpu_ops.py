@@ -243,6 +243,7 @@ def test_sequences_outside_the_cache_are_left_out():
     slot0, lens = i64([-16, 8, S, S - 16, 0]), i32([40, 40, 1, 17, -5])
     t = torch.ones((10, 1, 64), device=DEV, dtype=torch.float16)
     J.jet_qcache_write(p.gpu, slot0, lens, t, t, row_offsets=i32([0, 2, 4, 6, 8, 10]))
+    J.jet_qcache_write(p.gpu, i64([0, 0]), i32([2 ** 30 + 1, 2 ** 31 - 1]), t, t, row_offsets=i32([0, 2, 4]))
     J.jet_qcache_write(p.gpu, i64([0, 48]), i32([40, 40]), t, t, row_offsets=i32([2, 1, 11]))  # decreasing, past the rows
     J.jet_qcache_write(p.gpu, i64([0]), i32([40]), t, t, row_offsets=i32([-1, 1]))
     for a, b in zip(before, p.gpu.tensors):
@@ -680,3 +681,46 @@ def test_decode_steps_captured_and_replayed():
         for c, x in zip(caches, r):
             J.jet_qcache_read(c, slot0, i32(full), x[0], x[1], row_offsets=i32(offsets(full)))
         assert torch.equal(r[0][0], r[1][0]) and torch.equal(r[0][1], r[1][1])
+
+
+@pytest.mark.parametrize("rows,hd", [(1, 128), (40, 128), (40, 256), (7, 64)])
+def test_attention_captured_twice_from_one_workspace(rows, hd):
+    """Two graphs captured with the same workspace, replayed in turn with eager calls and synchronizations between."""
+    p, q = case(31, 0, 32, hd, 2, 4, [3000, 200], [rows, rows], "f16")
+    s0, ln, ro = i64(p.slot0), i32(p.lens), i32([0, rows, 2 * rows])
+    kw = dict(row_offsets=ro, max_rows=rows, max_len=3000)
+    want = J.jet_qcache_attention(p.gpu, s0, ln, q, torch.empty_like(q), **kw)
+    want2 = J.jet_qcache_attention(p.gpu, s0, ln, -q, torch.empty_like(q), causal=False, **kw)
+    ws = torch.empty(J.jet_qcache_attention_workspace(p.gpu, 2, 8, max_rows=rows, max_len=3000), dtype=torch.uint8,
+                     device=DEV)
+    q2, o1, o2 = -q, torch.empty_like(q), torch.empty_like(q)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1, stream=st):
+        J.jet_qcache_attention(p.gpu, s0, ln, q, o1, workspace=ws, **kw)
+    with torch.cuda.graph(g2, stream=st):
+        J.jet_qcache_attention(p.gpu, s0, ln, q2, o2, workspace=ws, causal=False, **kw)
+    for _ in range(3):
+        o1.zero_(), o2.zero_()
+        g1.replay()
+        g2.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o1, want) and torch.equal(o2, want2)
+        assert torch.equal(J.jet_qcache_attention(p.gpu, s0, ln, q, torch.empty_like(q), **kw), want)
+        torch.cuda.synchronize()
+
+
+def test_attention_of_no_rows_and_of_no_slots():
+    p, q = case(32, 0, 32, 64, 1, 2, [40], [3], "bf16")
+    none = q[:0]
+    assert J.jet_qcache_attention(p.gpu, i64([]), i32([]), none, none.clone(), row_offsets=i32([0])).shape[0] == 0
+    J.jet_qcache_write(p.gpu, i64([]), i32([]), q[:0, :1], q[:0, :1], row_offsets=i32([0]))
+    J.jet_qcache_attention(p.gpu, i64(p.slot0), i32(p.lens), none, none.clone(), row_offsets=i32([0, 0]))
+    empty = J.QCache.empty(1, 0, 64)
+    out = torch.full_like(q, 2.0)
+    J.jet_qcache_attention(empty, i64([0]), i32([0]), q, out, row_offsets=i32([0, 3]))
+    J.jet_qcache_write(empty, i64([0]), i32([0]), q[:, :1], q[:, :1], row_offsets=i32([0, 3]))
+    torch.cuda.synchronize()
+    assert torch.all(out == 2.0)  # no slot can be a sequence's first: it is left out
+    assert J.jet_logits_adjust(torch.empty((0, 50), device=DEV)).shape == (0, 50)

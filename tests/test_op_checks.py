@@ -102,6 +102,14 @@ def test_attention_arguments():
         assert got == J.JET_E_INVALID and msg, over
 
 
+def test_attention_of_too_many_heads_and_rows():
+    q = rows(row_stride=1 << 20)
+    got, msg = attention(cache(n_heads=1024), batch(), q, q, heads=32768 + 1024)
+    assert got == J.JET_E_INVALID and "heads" in msg
+    got, msg = attention(cache(n_heads=1), batch(n_rows=1 << 30), q, q, heads=2)
+    assert got == J.JET_E_INVALID and "n_rows" in msg
+
+
 def workspace(c, b, heads):
     n = ctypes.c_int64(-1)
     got, _ = call("jet_qcache_attention_workspace", c, b, heads, ctypes.byref(n))
