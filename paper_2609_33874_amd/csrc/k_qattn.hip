@@ -377,9 +377,11 @@ static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
     const int64_t step = kTile * kWaves, keys = ((len + n - 1) / n + step - 1) / step * step;
     return {few, (int)((len + keys - 1) / keys), keys};
   }
+  // (of eight waves, or 128 KB of LDS: one workgroup a CU)
+  const int64_t fill = block == 256 || c.hd == 256 ? kFill / 2 : kFill;
   int64_t best = INT64_MAX, at = 1;
   for (int64_t n = 1; n <= most; ++n) {
-    const int64_t cost = (units * n + kFill - 1) / kFill * ((len + n - 1) / n + kLeastKeys);
+    const int64_t cost = (units * n + fill - 1) / fill * ((len + n - 1) / n + kLeastKeys);
     if (cost < best) {
       best = cost;
       at = n;

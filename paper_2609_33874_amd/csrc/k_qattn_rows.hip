@@ -39,13 +39,13 @@ __device__ __forceinline__ Work work_of(int64_t w, int64_t units, int per) {
   return {w / 8 / per * 8 + w % 8, (int)(w / 8 % per)};
 }
 
-template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
-__global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAttn a, OwnRows own, int blocks,
+template <typename T, typename O, int FMT, int HD, int QB, bool OWN, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_rows_kernel(QAttn a, OwnRows own, int blocks,
                                                                            int nsplit) {
-  constexpr int NW = 4, KT = 64, BLOCK = 16 * QB * NW, NK = HD / 32, ND = HD / 16;
+  constexpr int KT = 64, NT = 64 * NW, BLOCK = 16 * QB * NW, NK = HD / 32, ND = HD / 16;
   constexpr int RB = HD * 2, CPR = HD / 8;                // bytes and 16-byte chunks of an f16 row
   constexpr int PLANE = KT * RB, STAGE = 2 * PLANE;       // K, then V
-  constexpr int RC = HD / 16, LD = KT * RC / (64 * NW);   // 16-byte chunks of an 8-bit row, and a thread's of a tile
+  constexpr int RC = HD / 16, LD = KT * RC / NT;   // 16-byte chunks of an 8-bit row, and a thread's of a tile
   extern __shared__ __align__(1024) char smem[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void *)smem;
@@ -141,13 +141,13 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
         const uint8_t *kt = K + (int64_t)t.t0 * HD, *vt = V + (int64_t)t.t0 * HD;
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
-          const uint32_t at = min(i * 4096 + (int)threadIdx.x * 16, t.nk * HD - 16);
+          const uint32_t at = min((i * NT + (int)threadIdx.x) * 16, t.nk * HD - 16);
           rk[i] = ld16(kt + at);
           rv[i] = ld16(vt + at);
         }
         re = scales[(t.t0 + min((here(threadIdx.x) & 3) * 16, t.nk - 1)) >> lb];
       };
-      // ... and from there into a stage. (A thread's next chunk lies 4096 / HD
+      // ... and from there into a stage. (A thread's next chunk lies 16 NT / HD
       // rows on, where the swizzle is the same; chunks c and c + 1 of its 16
       // values are neighbours in the swizzle too.)
       auto store = [&](int stage) {
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
         for (int i = 0; i < LD; ++i) {
           auto put = [&](uint32_t to, const uint4 &u) {
             const uint2 p = f16x4_of<FMT>(u.x), q = f16x4_of<FMT>(u.y), s = f16x4_of<FMT>(u.z), t = f16x4_of<FMT>(u.w);
-            *(lds_u32x4 *)(uintptr_t)(to + i * (4096 / HD) * RB) = u32x4{p.x, p.y, q.x, q.y};
-            *(lds_u32x4 *)(uintptr_t)((to ^ 16) + i * (4096 / HD) * RB) = u32x4{s.x, s.y, t.x, t.y};
+            *(lds_u32x4 *)(uintptr_t)(to + i * (NT * 16 / HD) * RB) = u32x4{p.x, p.y, q.x, q.y};
+            *(lds_u32x4 *)(uintptr_t)((to ^ 16) + i * (NT * 16 / HD) * RB) = u32x4{s.x, s.y, t.x, t.y};
           };
           put(ka, rk[i]);
           put(va, rv[i]);
@@ -464,16 +464,21 @@ __global__ __launch_bounds__(256, HD == 256 ? 1 : 2) void qattn_rows_kernel(QAtt
   }
 }
 
-// Query slots of a workgroup: 128, or 64 where no sequence has more (all four
-// waves have queries then: 8 KV heads, 16 sequences of 64 slots and 8192 keys, 113 us and
-// 91)
-// and of head_dim 256 (registers).
-int qattn_rows_block(int hd, int64_t slots) { return hd == 256 || slots <= 64 ? 64 : 128; }
+// Query slots of a workgroup: 64 where no sequence has more (all four waves have
+// queries then: 8 KV heads, 16 sequences of 64 slots and 8192 keys, 113 us with
+// blocks of 128, 91 with 64); from 256 on 256 in eight waves, which convert half
+// as many keys each (4 x 256 rows of 40 heads over 4096 .. 8192 keys: 216 us, 203
+// with 256). Of head_dim 256 half as many, a wave has registers for 16 queries; of
+// head_dim 64 no more than 128, a tile is one load of four waves.
+int qattn_rows_block(int hd, int64_t slots) {
+  if (hd == 256) return slots < 128 ? 64 : 128;
+  return slots <= 64 ? 64 : slots < 256 || hd == 64 ? 128 : 256;
+}
 
-template <typename T, typename O, int FMT, int HD, int QB, bool OWN>
+template <typename T, typename O, int FMT, int HD, int QB, bool OWN, int NW>
 static hipError_t run_rows(const QAttn &a, const OwnRows &own, int nsplit, hipStream_t st) {
-  constexpr int lds = 2 * 2 * 64 * HD * 2, BLOCK = 64 * QB;
-  const auto kernel = qattn_rows_kernel<T, O, FMT, HD, QB, OWN>;
+  constexpr int lds = 2 * 2 * 64 * HD * 2, BLOCK = 16 * QB * NW;
+  const auto kernel = qattn_rows_kernel<T, O, FMT, HD, QB, OWN, NW>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
@@ -481,20 +486,29 @@ static hipError_t run_rows(const QAttn &a, const OwnRows &own, int nsplit, hipSt
   const int64_t slots = (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H);
   const int blocks = (int)std::min<int64_t>((slots + BLOCK - 1) / BLOCK, 1 << 20);
   const int64_t total = OWN ? own.n_items : (int64_t)a.b.n_seq * a.c.H * blocks * nsplit;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(total, 1 << 20)), dim3(256), lds, st, a, own, blocks,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(total, 1 << 20)), dim3(64 * NW), lds, st, a, own, blocks,
                      nsplit);
   return hipGetLastError();
 }
 
+template <typename T, typename O, int FMT, int HD>
+static hipError_t rows_block(const QAttn &a, int nsplit, hipStream_t st) {
+  const int block = qattn_rows_block(HD, (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H));
+  if constexpr (HD == 256) {
+    return block == 64 ? run_rows<T, O, FMT, HD, 1, false, 4>(a, {}, nsplit, st)
+                       : run_rows<T, O, FMT, HD, 1, false, 8>(a, {}, nsplit, st);
+  } else {
+    if (block == 64) return run_rows<T, O, FMT, HD, 1, false, 4>(a, {}, nsplit, st);
+    if constexpr (HD == 128)
+      if (block == 256) return run_rows<T, O, FMT, HD, 2, false, 8>(a, {}, nsplit, st);
+    return run_rows<T, O, FMT, HD, 2, false, 4>(a, {}, nsplit, st);
+  }
+}
 template <typename T, typename O, int FMT>
 static hipError_t rows_hd(const QAttn &a, int nsplit, hipStream_t st) {
-  const bool half = qattn_rows_block(a.c.hd, (int64_t)std::max(a.b.max_rows, 1) * (a.Hq / a.c.H)) == 64;
-  if (a.c.hd == 64)
-    return half ? run_rows<T, O, FMT, 64, 1, false>(a, {}, nsplit, st) : run_rows<T, O, FMT, 64, 2, false>(a, {}, nsplit, st);
-  if (a.c.hd == 128)
-    return half ? run_rows<T, O, FMT, 128, 1, false>(a, {}, nsplit, st)
-                : run_rows<T, O, FMT, 128, 2, false>(a, {}, nsplit, st);
-  return run_rows<T, O, FMT, 256, 1, false>(a, {}, nsplit, st);
+  if (a.c.hd == 64) return rows_block<T, O, FMT, 64>(a, nsplit, st);
+  if (a.c.hd == 128) return rows_block<T, O, FMT, 128>(a, nsplit, st);
+  return rows_block<T, O, FMT, 256>(a, nsplit, st);
 }
 template <typename T, typename O> static hipError_t rows_fmt(const QAttn &a, int nsplit, hipStream_t st) {
   return a.c.fmt == 0 ? rows_hd<T, O, 0>(a, nsplit, st) : rows_hd<T, O, 1>(a, nsplit, st);
@@ -506,8 +520,8 @@ hipError_t launch_qattn_rows(const QAttn &a, int nsplit, hipStream_t st) {
 }
 
 template <int FMT, int HD> static hipError_t run_own(const QAttn &a, const OwnRows &own, hipStream_t st) {
-  if (own.block == 64) return run_rows<f16, f16, FMT, HD, 1, true>(a, own, 1, st);
-  if (own.block == 128) return run_rows<f16, f16, FMT, HD, 2, true>(a, own, 1, st);
+  if (own.block == 64) return run_rows<f16, f16, FMT, HD, 1, true, 4>(a, own, 1, st);
+  if (own.block == 128) return run_rows<f16, f16, FMT, HD, 2, true, 4>(a, own, 1, st);
   return hipErrorInvalidValue;
 }
 

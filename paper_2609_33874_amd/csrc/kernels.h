@@ -303,7 +303,7 @@ struct OwnRows {
   const void *K, *V;      // f16 [H][s_suf][hd]
   int64_t s_suf;
   const int32_t *row_n, *row_t;
-  int n_items, block;     // block: from qattn_rows_block
+  int n_items, block;     // block: from qattn_rows_block, at most 128
 };
 // Query slots of a workgroup where no sequence has more than `slots`.
 int qattn_rows_block(int hd, int64_t slots);

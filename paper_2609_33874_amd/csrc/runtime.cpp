@@ -718,7 +718,7 @@ Status plan_attention(jet_model *m, int mode, const QDesc &qd, const char *tag, 
   for (auto n : qd.nrows)
     if (n > 0) slots += (double)G * n, nq += 1, widest = std::max(widest, (int64_t)G * n);
   const int block = own_cache
-                        ? jetk::qattn_rows_block((int)h.head_dim, widest)
+                        ? std::min(jetk::qattn_rows_block((int)h.head_dim, widest), 128)
                         : jetk::attn_block(m->kdt, m->apair, mode, nq > 0 ? slots / nq : 0, slots * (double)h.n_kv_heads);
   build_items(qd, G, (int)h.n_kv_heads, mode == 0, block, &items, &pairs);
   // Longest work first: the dispatcher hands out workgroups in order, so long
