@@ -15,24 +15,28 @@
 
 namespace jetk {
 
-// Eight consecutive values of a row from element i.
-template <typename T, bool VEC> __device__ __forceinline__ void load8(float (&x)[8], const T *p) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    const uint4 u = ld16(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// Eight consecutive values of a row as they lie in memory, and as floats.
+template <typename T> struct Raw8 {
+  uint4 u[sizeof(T) / 2];
+};
+template <typename T, bool VEC> __device__ __forceinline__ Raw8<T> load8(const T *p) {
+  Raw8<T> r;
+  if constexpr (VEC) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] & 0xffff)));
-      x[2 * j + 1] = to_f<T>(__builtin_bit_cast(T, (uint16_t)(w[j] >> 16)));
-    }
-  } else if constexpr (VEC) {
-    const uint4 u = ld16(p), w = ld16(p + 4);
-    x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
-    x[4] = __uint_as_float(w.x); x[5] = __uint_as_float(w.y); x[6] = __uint_as_float(w.z); x[7] = __uint_as_float(w.w);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.u[i] = ld16(p + i * 16 / sizeof(T));
   } else {
+    T x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = to_f<T>(p[j]);
+    for (int j = 0; j < 8; ++j) x[j] = p[j];
+    __builtin_memcpy(&r, x, sizeof(r));
   }
+  return r;
+}
+template <typename T> __device__ __forceinline__ void floats8(float (&x)[8], const Raw8<T> &r) {
+  T t[8];
+  __builtin_memcpy(t, &r, sizeof(r));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = to_f<T>(t[j]);
 }
 template <typename T, bool VEC> __device__ __forceinline__ void store8(T *p, const float (&x)[8]) {
   if constexpr (VEC && sizeof(T) == 2) {
@@ -51,15 +55,17 @@ template <int FMT> __device__ __forceinline__ void unpack8x8(float (&x)[8], uint
 }
 
 // One workgroup per (block that a sequence's rows touch, head of K or of V,
-// sequence): it owns the block, so nothing is shared between workgroups.
-template <typename T, int FMT, bool VEC>
+// sequence): it owns the block, so nothing is shared between workgroups. A
+// thread holds NC pieces of eight values between the two passes over them
+// (maximum, rounding); blocks of more values than that are read twice.
+template <typename T, int FMT, bool VEC, int NC>
 __global__ __launch_bounds__(256) void qcache_write_kernel(QCache c, QBatch b, QRows rk, QRows rv) {
   __shared__ uint32_t wmax[4];
   const int tid = threadIdx.x, h = blockIdx.y >> 1;
   const bool isv = blockIdx.y & 1;
   const QSeq s = qseq(b, c, blockIdx.z);
   if (s.lo >= s.hi) return;
-  const int B = 1 << c.lb, hd = c.hd, cpr = hd / 8;  // chunks of 8 values per row
+  const int B = 1 << c.lb, hd = c.hd, lc = __builtin_ctz(hd) - 3, cpr = 1 << lc;  // pieces per row
   const QRows &r = isv ? rv : rk;
   uint8_t *data = (isv ? c.v : c.k) + ((int64_t)h * c.S + s.slot0) * hd;
   uint8_t *exps = (isv ? c.ve : c.ke) + (int64_t)h * (c.S >> c.lb) + (s.slot0 >> c.lb);
@@ -67,29 +73,43 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(QCache c, QBatch b, Q
   for (int blk = b0 + blockIdx.x; blk <= b1; blk += gridDim.x) {
     const int first = blk << c.lb, lo = max(s.lo, first), hi = min(s.hi, first + B);  // the block's new tokens
     const T *src = (const T *)r.p + (int64_t)(s.row0 + lo - s.pos0) * r.rs + (int64_t)h * r.hs;
-    const int n = (hi - lo) * cpr;
+    const int n = (hi - lo) << lc;
+    auto piece = [&](int i) { return load8<T, VEC>(src + (int64_t)(i >> lc) * r.rs + (i & (cpr - 1)) * 8); };
     uint32_t top = 0;  // float bits of |x| order like the values, NaN and infinity above all
-    for (int i = tid; i < n; i += 256) {
+    auto raise = [&](const Raw8<T> &p) {
       float x[8];
-      load8<T, VEC>(x, src + (int64_t)(i / cpr) * r.rs + i % cpr * 8);
+      floats8<T>(x, p);
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-    }
+    };
+    const int old = lo > first ? exps[blk] : 0;  // scale byte of the block's earlier tokens
+    Raw8<T> held[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+      if (k * 256 + tid < n) held[k] = piece(k * 256 + tid);
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+      if (k * 256 + tid < n) raise(held[k]);
+    for (int i = NC * 256 + tid; i < n; i += 256) raise(piece(i));
     for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     if ((tid & 63) == 0) wmax[tid >> 6] = top;
-    const int old = lo > first ? exps[blk] : 0;  // scale byte of the block's earlier tokens
     __syncthreads();
     top = max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3]));
     const int e = max(scale_byte<FMT>(top), old);
     const float down = e == kExpNaN ? 0.0f : pow2i(kExpBias - e);
-    for (int i = tid; i < n; i += 256) {
+    uint8_t *dst = data + (int64_t)lo * hd;
+    auto put = [&](int i, const Raw8<T> &p) {
       float x[8];
-      load8<T, VEC>(x, src + (int64_t)(i / cpr) * r.rs + i % cpr * 8);
+      floats8<T>(x, p);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = e == kExpNaN ? 0.0f : x[j] * down;
-      uint2 w = make_uint2(pack8x4<FMT>(x[0], x[1], x[2], x[3]), pack8x4<FMT>(x[4], x[5], x[6], x[7]));
-      *reinterpret_cast<uint2 *>(data + (int64_t)lo * hd + (int64_t)i * 8) = w;
-    }
+      *reinterpret_cast<uint2 *>(dst + (int64_t)i * 8) =
+          make_uint2(pack8x4<FMT>(x[0], x[1], x[2], x[3]), pack8x4<FMT>(x[4], x[5], x[6], x[7]));
+    };
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+      if (k * 256 + tid < n) put(k * 256 + tid, held[k]);
+    for (int i = NC * 256 + tid; i < n; i += 256) put(i, piece(i));
     if (e > old && lo > first && e != kExpNaN) {  // the earlier tokens' scale grew
       for (int i = tid; i < (lo - first) * cpr; i += 256) {
         uint2 *p = reinterpret_cast<uint2 *>(data + (int64_t)first * hd + (int64_t)i * 8);
@@ -112,14 +132,14 @@ __global__ __launch_bounds__(256) void qcache_read_kernel(QCache c, QBatch b, QR
   const int tid = threadIdx.x, h = blockIdx.y >> 1;
   const bool isv = blockIdx.y & 1;
   const QSeq s = qseq(b, c, blockIdx.z);
-  const int hd = c.hd, cpr = hd / 8;
+  const int hd = c.hd, lc = __builtin_ctz(hd) - 3;  // log2 of the pieces of eight values in a row
   const QRows &r = isv ? rv : rk;
   const uint8_t *data = (isv ? c.v : c.k) + ((int64_t)h * c.S + s.slot0) * hd;
   const uint8_t *exps = (isv ? c.ve : c.ke) + (int64_t)h * (c.S >> c.lb) + (s.slot0 >> c.lb);
   for (int64_t t0 = s.lo + (int64_t)blockIdx.x * kReadTokens; t0 < s.hi; t0 += (int64_t)gridDim.x * kReadTokens) {
-    const int n = min(kReadTokens, s.hi - (int)t0) * cpr;
+    const int n = min(kReadTokens, s.hi - (int)t0) << lc;
     for (int i = tid; i < n; i += 256) {
-      const int t = (int)t0 + i / cpr, d = i % cpr * 8;
+      const int t = (int)t0 + (i >> lc), d = (i & ((1 << lc) - 1)) * 8;
       const int e = exps[t >> c.lb];
       float x[8];
       unpack8x8<FMT>(x, *reinterpret_cast<const uint2 *>(data + (int64_t)t * hd + d));
@@ -133,27 +153,34 @@ __global__ __launch_bounds__(256) void qcache_read_kernel(QCache c, QBatch b, QR
 
 // Launch over (x, head of K or V, sequence); kernels walk on where a sequence
 // has more rows than the grid was sized for.
-#define JETK_QROWS(KERNEL)                                                                                        \
-  do {                                                                                                            \
-    const bool vec = k.vec && v.vec;                                                                              \
-    if (c.fmt == 0 && vec) hipLaunchKernelGGL((KERNEL<T, 0, true>), grid, dim3(256), 0, st, c, b, k, v);          \
-    else if (c.fmt == 0) hipLaunchKernelGGL((KERNEL<T, 0, false>), grid, dim3(256), 0, st, c, b, k, v);           \
-    else if (vec) hipLaunchKernelGGL((KERNEL<T, 1, true>), grid, dim3(256), 0, st, c, b, k, v);                   \
-    else hipLaunchKernelGGL((KERNEL<T, 1, false>), grid, dim3(256), 0, st, c, b, k, v);                           \
-  } while (0)
-
+template <typename T, int NC>
+static void write_nc(dim3 grid, const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
+  const bool vec = k.vec && v.vec;
+  if (c.fmt == 0 && vec) hipLaunchKernelGGL((qcache_write_kernel<T, 0, true, NC>), grid, dim3(256), 0, st, c, b, k, v);
+  else if (c.fmt == 0) hipLaunchKernelGGL((qcache_write_kernel<T, 0, false, NC>), grid, dim3(256), 0, st, c, b, k, v);
+  else if (vec) hipLaunchKernelGGL((qcache_write_kernel<T, 1, true, NC>), grid, dim3(256), 0, st, c, b, k, v);
+  else hipLaunchKernelGGL((qcache_write_kernel<T, 1, false, NC>), grid, dim3(256), 0, st, c, b, k, v);
+}
 template <typename T>
 static hipError_t write_t(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
-  const int64_t blocks = ((int64_t)std::max(b.max_rows, 1) + (1 << c.lb) - 2) / (1 << c.lb) + 1;
+  const int64_t rows = std::max(b.max_rows, 1), blocks = (rows + (1 << c.lb) - 2) / (1 << c.lb) + 1;
   const dim3 grid((unsigned)std::min<int64_t>(blocks, 65536), (unsigned)(2 * c.H), (unsigned)b.n_seq);
-  JETK_QROWS(qcache_write_kernel);
+  // pieces of eight values in a block's new rows
+  const int64_t pieces = std::min<int64_t>(rows, 1 << c.lb) * c.hd / 8;
+  if (pieces <= 256) write_nc<T, 1>(grid, c, b, k, v, st);
+  else if (pieces <= 512) write_nc<T, 2>(grid, c, b, k, v, st);
+  else write_nc<T, 4>(grid, c, b, k, v, st);
   return hipGetLastError();
 }
 template <typename T>
 static hipError_t read_t(const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
   const int64_t runs = ((int64_t)std::max(b.max_rows, 1) + kReadTokens - 1) / kReadTokens;
   const dim3 grid((unsigned)std::min<int64_t>(runs, 65536), (unsigned)(2 * c.H), (unsigned)b.n_seq);
-  JETK_QROWS(qcache_read_kernel);
+  const bool vec = k.vec && v.vec;
+  if (c.fmt == 0 && vec) hipLaunchKernelGGL((qcache_read_kernel<T, 0, true>), grid, dim3(256), 0, st, c, b, k, v);
+  else if (c.fmt == 0) hipLaunchKernelGGL((qcache_read_kernel<T, 0, false>), grid, dim3(256), 0, st, c, b, k, v);
+  else if (vec) hipLaunchKernelGGL((qcache_read_kernel<T, 1, true>), grid, dim3(256), 0, st, c, b, k, v);
+  else hipLaunchKernelGGL((qcache_read_kernel<T, 1, false>), grid, dim3(256), 0, st, c, b, k, v);
   return hipGetLastError();
 }
 
