@@ -1,5 +1,14 @@
 // Attention over a cache held in 8 bits (jet.h: jet_qcache_attention).
 // Few query slots: see qattn.h for the arithmetic, k_qattn_rows.hip for many.
+//
+// Bound by reading the cache once, 2 hd + a little bytes a key and KV head, while
+// the matrix cores take at most 32 queries against each (a wave needs 16 at
+// least: of one question's five or six heads of a group the rest are idle).
+// 16 questions of 65536 .. 131072 keys, 8 KV heads of 128: 3.24 GB in 566 us, 5.7
+// TB/s of the 6.4 that a kernel of plain reads reaches; 64 of 1024 .. 4096 keys 4.6
+// TB/s in a single round of unequal workgroups; one question's 731 keys 10 us,
+// which is latency (a tile's loads, products and softmax one after another, three
+// tiles a wave, the joining in LDS).
 #include <algorithm>
 
 #include "qattn.h"
@@ -38,7 +47,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 }
 
 // One workgroup per (block of 16 QB query slots and split of the keys, KV
-// head, sequence); slot = row * G + head. Each wave takes every fourth tile of
+// head, sequence); slot = row * G + head. Each wave takes every eighth tile of
 // 32 keys of the split on its own (K and V go straight into registers as the
 // matrix cores take them, the next tile's on their way meanwhile), and the
 // waves' results are joined in LDS.

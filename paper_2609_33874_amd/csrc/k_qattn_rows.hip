@@ -1,13 +1,18 @@
 // Attention over a cache held in 8 bits, many query slots: see qattn.h for the
-// arithmetic. A workgroup of four waves takes 64 QB query slots of one
-// (sequence, KV head); tiles of 64 keys are turned into f16 once for all of
-// them on their way into LDS (two stages: while one is computed the next one
+// arithmetic. A workgroup of four or eight waves takes 16 QB query slots a wave
+// of one (sequence, KV head); tiles of 64 keys are turned into f16 once for all
+// of them on their way into LDS (two stages: while one is computed the next one
 // is converted and the one after it loaded into registers), so that per key
-// tile and wave the conversion is a quarter of what it would be in the waves'
-// own registers, where it costs more than the products.
-// What bounds it: the vector instructions of the softmax (about six and an
-// exponential per score) and the LDS reads of K and V, each about as long as
-// the matrix instructions.
+// tile and wave the conversion is a quarter or an eighth of what it would be in
+// the waves' own registers, where it costs more than the products.
+// What bounds it: 4 x 256 rows of 40 heads (8 KV heads of 128) over 4096 .. 8192
+// keys take 204 us (0.59 PFLOP/s; a large library product of f16 reaches 1.15), of
+// which the vector instructions of the softmax and the conversion (430 a tile and
+// wave of 32 queries) are about 100 us, the matrix instructions 48 and the LDS
+// reads of K and V 48: two waves a SIMD hide little of one behind the other.
+// (Half of the waves converting after their products instead of before: 227 us;
+// wave priorities for the products, or for the softmax: 204; 16 queries a wave and
+// four waves a SIMD, which read K and V twice as often from LDS: 202.)
 // With own rows (candidate scoring) the keys of a query's own candidate follow
 // as 16-bit tiles of the same stream; there no split is made and every query
 // runs the same operations in the same order whatever block it lies in.

@@ -8,7 +8,11 @@
 //   e = max(e, e_old) and, if it grew, q_old = rne(q_old 2^(e_old - e)).
 // 2^-e is exact, so every value is rounded once; an earlier value that goes
 // through several growths is off by less than 2^e (1/2 + 1/4 + ... steps).
-// Memory bound: rows read once, one byte written for each value.
+// Memory bound: rows read once, one byte written for each value, and the other
+// way round to read. 36400 bf16 tokens of 8 heads of 128 in blocks of 64, K and V
+// (224 MB either way): written in 57 us (3.9 TB/s), read back in 37 (6.0 TB/s, a
+// part from the last-level cache, where the write left it). 164000 tokens read as
+// f16 (1.0 GB): 183 us, 5.5 TB/s. A large copy moves 4.7 TB/s.
 #include <algorithm>
 
 #include "qcache.h"
@@ -57,7 +61,8 @@ template <int FMT> __device__ __forceinline__ void unpack8x8(float (&x)[8], uint
 // One workgroup per (block that a sequence's rows touch, head of K or of V,
 // sequence): it owns the block, so nothing is shared between workgroups. A
 // thread holds NC pieces of eight values between the two passes over them
-// (maximum, rounding); blocks of more values than that are read twice.
+// (maximum, rounding); blocks of more values than that are read twice (the rows
+// above: 62 us with every block read twice, from L2 the second time, 57 held).
 template <typename T, int FMT, bool VEC, int NC>
 __global__ __launch_bounds__(256) void qcache_write_kernel(QCache c, QBatch b, QRows rk, QRows rv) {
   __shared__ uint32_t wmax[4];
@@ -125,7 +130,8 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(QCache c, QBatch b, Q
   }
 }
 
-// One workgroup per (run of tokens, head of K or of V, sequence).
+// One workgroup per (run of tokens, head of K or of V, sequence). (Sizes are
+// powers of two: shifts. Divisions by them cost the read above 42 us for 37.)
 constexpr int kReadTokens = 32;
 template <typename T, int FMT, bool VEC>
 __global__ __launch_bounds__(256) void qcache_read_kernel(QCache c, QBatch b, QRows rk, QRows rv) {
@@ -152,7 +158,8 @@ __global__ __launch_bounds__(256) void qcache_read_kernel(QCache c, QBatch b, QR
 }
 
 // Launch over (x, head of K or V, sequence); kernels walk on where a sequence
-// has more rows than the grid was sized for.
+// has more rows than the grid was sized for. NC by the values of a whole block's
+// new rows, so that appended tokens hold no idle pieces.
 template <typename T, int NC>
 static void write_nc(dim3 grid, const QCache &c, const QBatch &b, const QRows &k, const QRows &v, hipStream_t st) {
   const bool vec = k.vec && v.vec;
