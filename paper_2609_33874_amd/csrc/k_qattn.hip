@@ -374,7 +374,8 @@ struct Plan {
 // has no registers for them, and reads its keys again).
 static int few_block(int hd, int64_t slots) { return slots > 16 && hd < 256 ? 32 : 16; }
 static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
-  const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H), len = std::min(std::max<int64_t>(b.max_len, 1), (int64_t)1 << 30);
+  const int64_t slots = (int64_t)std::max(b.max_rows, 1) * (Hq / c.H);
+  const int64_t len = std::min(std::max<int64_t>(b.max_len, 1), (int64_t)1 << 30);
   const bool few = slots <= kFewSlots;
   const int64_t block = few ? few_block(c.hd, slots) : qattn_rows_block(c.hd, slots);
   const int64_t units = (int64_t)std::max(b.n_seq, 1) * c.H * ((slots + block - 1) / block);
@@ -388,9 +389,10 @@ static Plan plan_of(const QCache &c, const QBatch &b, int Hq) {
   }
   // (of eight waves, or 128 KB of LDS: one workgroup a CU)
   const int64_t fill = block == 256 || c.hd == 256 ? kFill / 2 : kFill;
-  int64_t best = INT64_MAX, at = 1;
+  double best = INFINITY;  // (whole numbers of 64 bits could overflow)
+  int64_t at = 1;
   for (int64_t n = 1; n <= most; ++n) {
-    const int64_t cost = (units * n + fill - 1) / fill * ((len + n - 1) / n + kLeastKeys);
+    const double cost = (double)((units * n + fill - 1) / fill) * (double)((len + n - 1) / n + kLeastKeys);
     if (cost < best) {
       best = cost;
       at = n;

@@ -3,6 +3,7 @@
 // work is enqueued on the caller's stream.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <exception>
 #include <string>
 
@@ -59,8 +60,9 @@ jetk::QCache cache_of(const jet_qcache &c) {
   const int lb = c.block == 16 ? 4 : c.block == 32 ? 5 : c.block == 64 ? 6 : 7;
   return {c.format, lb, c.n_heads, c.head_dim, c.n_slots, (uint8_t *)c.k, (uint8_t *)c.v, c.k_exp, c.v_exp};
 }
-jetk::QBatch batch_of(const jet_qcache_batch &b) {
-  return {b.n_seq, b.n_rows, b.max_rows, b.max_len, b.slot0, b.len, b.row_offsets};
+// (no sequence has more rows than the call, or more tokens than the cache)
+jetk::QBatch batch_of(const jet_qcache_batch &b, const jet_qcache &c) {
+  return {b.n_seq, b.n_rows, std::min(b.max_rows, b.n_rows), std::min(b.max_len, c.n_slots), b.slot0, b.len, b.row_offsets};
 }
 jetk::QRows rows_of(const jet_rows &r) { return {r.p, r.type, rows_aligned(r) ? 1 : 0, r.row_stride, r.head_stride}; }
 
@@ -95,9 +97,9 @@ Status move_rows(bool write, const jet_qcache *c, const jet_qcache_batch *b, con
   if (b->n_seq == 0 || b->n_rows == 0 || c->n_slots == 0) return Status::ok();
   OnDeviceOf dev(c->k, st);
   TRY(dev.st);
-  if (write) return launched(jetk::launch_qcache_write(cache_of(*c), batch_of(*b), rows_of(*k), rows_of(*v), st),
+  if (write) return launched(jetk::launch_qcache_write(cache_of(*c), batch_of(*b, *c), rows_of(*k), rows_of(*v), st),
                              "jet_qcache_write");
-  return launched(jetk::launch_qcache_read(cache_of(*c), batch_of(*b), rows_of(*k), rows_of(*v), st),
+  return launched(jetk::launch_qcache_read(cache_of(*c), batch_of(*b, *c), rows_of(*k), rows_of(*v), st),
                   "jet_qcache_read");
 }
 
@@ -113,7 +115,7 @@ Status attention(const jet_qcache *c, const jet_qcache_batch *b, int32_t n_q_hea
     return Status::err(JET_E_INVALID, "n_rows times the query heads of a KV head exceeds 2^30");
   if ((uintptr_t)lse % 4) return Status::err(JET_E_INVALID, "lse is not aligned");
   const jetk::QCache qc = cache_of(*c);
-  const jetk::QBatch qb = batch_of(*b);
+  const jetk::QBatch qb = batch_of(*b, *c);
   const int64_t need = jetk::qattn_workspace(qc, qb, n_q_heads);
   if (need > 0 && (!ws || ws_bytes < need || (uintptr_t)ws % 16))
     return Status::err(JET_E_INVALID, "workspace: " + std::to_string(need) + " bytes needed, 16-byte aligned");
@@ -166,7 +168,7 @@ extern "C" int jet_qcache_attention_workspace(const jet_qcache *cache, const jet
     TRY(check_qcache(cache));
     TRY(check_batch_counts(batch));
     TRY(check_q_heads(cache, n_q_heads, 1.0f));
-    *out_bytes = jetk::qattn_workspace(cache_of(*cache), batch_of(*batch), n_q_heads);
+    *out_bytes = jetk::qattn_workspace(cache_of(*cache), batch_of(*batch, *cache), n_q_heads);
     return Status::ok();
   });
 }

@@ -479,6 +479,10 @@ def _move_rows(fn, cache, slot0, length, k, v, row_offsets, max_rows, stream):
     rk, rv, n = _rows(k, "k", H, hd, dev), _rows(v, "v", H, hd, dev), k.shape[0]
     if n != v.shape[0]:
         raise ValueError("k and v have different numbers of rows")
+    if max_rows is None and row_offsets is not None:
+        # (kernels walk on in a longer sequence; a launch for n rows of every
+        # sequence would mostly be workgroups without any)
+        max_rows = min(n, 2 * n // max(slot0.shape[0], 1) + 1)
     # (structs are passed by reference: ctypes does that itself for a POINTER argument)
     _check(fn(c, _batch(cache, slot0, length, n, row_offsets, max_rows, None), rk, rv, _stream(stream, dev)))
 
@@ -486,12 +490,15 @@ def _move_rows(fn, cache, slot0, length, k, v, row_offsets, max_rows, stream):
 def jet_qcache_write(cache: QCache, slot0, length, k, v, row_offsets=None, max_rows=None, stream=None) -> None:
     """Quantises rows of k and v ([rows, heads, head_dim]) into the cache: the
     last tokens of each sequence (slot0 int64, length int32, both [n_seq];
-    row_offsets int32 [n_seq + 1], None: one row each)."""
+    row_offsets int32 [n_seq + 1], None: one row each). max_rows: most rows of
+    a sequence, which sizes the launch (None: about twice their mean; a longer
+    sequence is worked off all the same)."""
     _move_rows(lib().jet_qcache_write, cache, slot0, length, k, v, row_offsets, max_rows, stream)
 
 
 def jet_qcache_read(cache: QCache, slot0, length, k, v, row_offsets=None, max_rows=None, stream=None) -> None:
-    """Reads the last tokens of each sequence back into the rows of k and v."""
+    """Reads the last tokens of each sequence back into the rows of k and v
+    (arguments as jet_qcache_write's)."""
     _move_rows(lib().jet_qcache_read, cache, slot0, length, k, v, row_offsets, max_rows, stream)
 
 
@@ -510,7 +517,9 @@ def jet_qcache_attention(cache: QCache, slot0, length, q, out, row_offsets=None,
     """Attention of q ([rows, n_q_heads, head_dim], float16 or bfloat16) over the
     cache into `out` (q's type or float32), the rows being the last tokens of
     each sequence; lse: float32 [rows, n_q_heads] or None. scale: 1 /
-    sqrt(head_dim) by default. workspace: a uint8 tensor of at least
+    sqrt(head_dim) by default. max_rows, max_len: most rows and tokens of one
+    sequence, by which the kernel and its launch are chosen (None: all rows, one
+    where there are no row_offsets, and all slots). workspace: a uint8 tensor of at least
     jet_qcache_attention_workspace bytes (None: one is allocated). Returns out."""
     c, dev, L, torch = cache.c, cache.device, lib(), _t()[0]
     hd, shape = c.head_dim, q.shape
@@ -572,8 +581,8 @@ def jet_logits_adjust(logits, out=None, history=None, hist_prompt=None, repetiti
         a.bias_ids, a.n_bias = _device_array(bias[1], "bias ids", i32, dev), bias[1].numel()
         a.bias_values = _device_array(bias[2], "bias values", f32, dev, (a.n_bias,))
     if masks is not None:
-        if masks.dim() != 2:
-            raise ValueError("masks must be [n_masks, words]")
+        if masks.dim() != 2 or (R and not masks.shape[0]):
+            raise ValueError("masks must be [n_masks, words], one mask at least")
         a.masks, a.n_masks = _device_array(masks, "masks", i32, dev), masks.shape[0]
         a.mask_stride = masks.shape[1]
     a.mask_index = _device_array(mask_index, "mask_index", i32, dev, (R,))

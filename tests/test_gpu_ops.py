@@ -617,6 +617,37 @@ def test_logits_offsets_outside_their_lists():
     assert torch.equal(out, want)
 
 
+def test_an_empty_list_of_masks_is_refused():
+    x = torch.zeros((3, 40), device="cuda")
+    none = torch.empty((0, 2), dtype=torch.int32, device="cuda")
+    index = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for kw in ({}, {"mask_index": index}):
+        with pytest.raises(ValueError):
+            J.jet_logits_adjust(x, masks=none, **kw)
+
+
+def test_rows_of_very_unequal_sequences():
+    """Without max_rows the launch is sized by the mean: one sequence far above it."""
+    H, hd, block, lens = 2, 128, 32, [3, 900, 1, 0, 40, 2, 5, 1]
+    off = np.concatenate([[0], np.cumsum(lens)])
+    slot0 = np.concatenate([[0], np.cumsum([(n + block - 1) // block * block for n in lens])])
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((int(off[-1]), H, hd), generator=g).to(torch.float16).cuda() for _ in "kv")
+    cache = J.QCache.empty(H, int(slot0[-1]), hd, block)
+    args = (torch.tensor(slot0[:-1], dtype=torch.int64).cuda(), torch.tensor(lens, dtype=torch.int32).cuda())
+    kw = {"row_offsets": torch.tensor(off, dtype=torch.int32).cuda()}
+    J.jet_qcache_write(cache, *args, k, v, **kw)
+    a, b = (torch.empty((int(off[-1]), H, hd), device="cuda") for _ in "kv")
+    J.jet_qcache_read(cache, *args, a, b, **kw)
+    for x, y in ((k, a), (v, b)):
+        for s, n in enumerate(lens):
+            for t in range(0, n, block):
+                i = slice(int(off[s]) + t, int(off[s]) + min(t + block, n))
+                # the scale is at most twice what the block's maximum needs: half a step
+                top = x[i].float().abs().amax(dim=(0, 2), keepdim=True)
+                assert ((x[i].float() - y[i]).abs() <= top / 127).all()
+
+
 def test_logits_of_many_rows():
     """More rows than one launch's grid, short vocabularies."""
     R, V = 70000, 5
