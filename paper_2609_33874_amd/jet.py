@@ -533,9 +533,14 @@ def jet_qcache_attention(cache: QCache, slot0, length, q, out, row_offsets=None,
         n = ctypes.c_int64()
         _check(L.jet_qcache_attention_workspace(c, b, Hq, n))
         if n.value:
-            workspace = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{dev}")
-            if stream is not None:  # keep its memory until that stream's work is done
-                workspace.record_stream(torch.cuda.ExternalStream(stream, device=dev))
+            if stream is None or stream == _stream(None, dev):
+                workspace = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{dev}")
+            else:
+                # out of that stream's pool: a block that was freed on the current
+                # one may still be in use by work that is queued there
+                with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=dev) if stream
+                                       else torch.cuda.default_stream(dev)):
+                    workspace = torch.empty(n.value, dtype=torch.uint8, device=f"cuda:{dev}")
     ws, ws_n = (None, 0) if workspace is None else (_device_array(workspace, "workspace", torch.uint8, dev),
                                                     workspace.numel())
     _check(L.jet_qcache_attention(c, b, Hq, hd ** -0.5 if scale is None else scale, 1 if causal else 0, rq, ro,
