@@ -13,7 +13,8 @@ __global__ __launch_bounds__(256) void embed_kernel(const T *__restrict__ E, con
                                                      const int32_t *__restrict__ idx, int d,
                                                      float *__restrict__ resid) {
   const int r = blockIdx.x;
-  const int64_t tok = ids[idx ? idx[r] : r];
+  // -1 where a trace's sampling found no token (the call ends in an error): any row will do
+  const int64_t tok = max(ids[idx ? idx[r] : r], 0);
   const T *src = E + tok * d;
   float *dst = resid + (int64_t)r * d;
   for (int i = threadIdx.x; i < d; i += 256) dst[i] = to_f<T>(src[i]);

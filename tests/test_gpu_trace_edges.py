@@ -1,0 +1,40 @@
+"""GPU: traces whose logits leave nothing to sample, and rules at their edges."""
+import numpy as np
+import pytest
+
+import jet_synth
+from paper_2609_33874_amd import jet as J
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def nan_model(tmp_path_factory):
+    """A model whose every logit is NaN."""
+    path = str(tmp_path_factory.mktemp("nan") / "nan.jetm")
+    header = jet_synth.write_model(path, "small_gqa_bf16")
+    t = next(t for t in header["tensors"] if t["name"] == "final_norm")
+    w = np.memmap(path, dtype=np.float32, mode="r+", offset=t["offset"], shape=tuple(t["shape"]))
+    w[:] = np.nan
+    w.flush()
+    return path
+
+
+@pytest.mark.parametrize("flags", [0, J.JET_FLAG_QCACHE_INT8])
+@pytest.mark.parametrize("dtype", [J.JET_FP32, J.JET_F16])
+@pytest.mark.parametrize("rules", [False, True])
+def test_logits_that_are_not_numbers_end_the_trace(dtype, flags, rules, nan_model):
+    """No token is found (-1), at the first of several steps: the call fails and later steps read no embedding of it."""
+    wl = jet_synth.make_workload("small", n_questions=2)
+    m = J.jet_model_load(nan_model, dtype=dtype, flags=flags)
+    try:
+        p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+        with pytest.raises(J.JetError) as e:
+            if rules:
+                J.jet_generate_trace_rules(m, p, 2, 3, 0.7, 1, repetition=1.2)
+            else:
+                J.jet_generate_trace(m, p, 2, 3, 0.7, 1)
+        assert e.value.code == J.JET_E_DEVICE and "finite" in str(e.value)
+        J.jet_prefix_free(p)
+    finally:
+        J.jet_model_free(m)
