@@ -225,7 +225,8 @@ typedef struct {
  * jet_generate_trace_rules - jet_generate_trace with rules: the logits of every
  * step are adjusted before its token is sampled. rules NULL: none.
  * Errors: as jet_generate_trace; JET_E_INVALID also for malformed rules
- *   (nothing has changed then).
+ *   (nothing has changed then), JET_E_DEVICE also where no token that a step
+ *   allows has a logit above -inf (penalties can overflow), as without rules.
  */
 int jet_generate_trace_rules(jet_model *model, jet_prefix *prefix, int32_t n_steps, float temperature, uint64_t seed,
                              const jet_trace_rules *rules, int32_t *out_tokens);

@@ -439,7 +439,9 @@ __device__ __forceinline__ double gumbel_at(uint64_t seed, int q, int t, int v) 
 
 // Row r, slice y of the vocabulary (gridDim.y slices): the slice's largest
 // key_v = z_v / tau + G_v (tau > 0) or z_v (tau = 0) and its token, the
-// lowest v among equal keys, v = -1 if no key is a number.
+// lowest v among equal keys, v = -1 if no key is a number above -inf (a token
+// that a mask forbids has -inf, and must not win where penalties or a NaN leave
+// the allowed ones nothing).
 constexpr int kSampleSplit = 32;
 
 __global__ __launch_bounds__(256) void sample_part_kernel(const float *__restrict__ logits, int64_t ldl, int V,
@@ -454,7 +456,7 @@ __global__ __launch_bounds__(256) void sample_part_kernel(const float *__restric
   int arg = -1;
   for (int v = v0 + tid; v < v1; v += 256) {
     const double key = tau > 0.0 ? (double)z[v] / tau + gumbel_at(seed, q0 + r, t, v) : (double)z[v];
-    if (key == key && (arg < 0 || key > best)) {  // v ascends: equal keys keep the lower v
+    if (key > -INFINITY && (arg < 0 || key > best)) {  // v ascends: equal keys keep the lower v
       best = key;
       arg = v;
     }

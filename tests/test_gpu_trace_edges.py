@@ -38,3 +38,27 @@ def test_logits_that_are_not_numbers_end_the_trace(dtype, flags, rules, nan_mode
         J.jet_prefix_free(p)
     finally:
         J.jet_model_free(m)
+
+
+@pytest.mark.parametrize("tau", [0.0, 0.8])
+@pytest.mark.parametrize("flags", [0, J.JET_FLAG_QCACHE_INT8])
+def test_a_forbidden_token_is_never_sampled(flags, tau, model_dir):
+    """One allowed token whose penalty overflows at its third time: the step has no token, not the lowest forbidden one."""
+    path = jet_synth.ensure_model("small_gqa_bf16", cache_dir=model_dir)
+    wl = jet_synth.make_workload("small", n_questions=2)
+    words = np.zeros((1, (3000 + 31) // 32), np.uint32)
+    words[0, 17 // 32] = 1 << 17 % 32
+    m = J.jet_model_load(path, dtype=J.JET_F16, flags=flags)
+    try:
+        for n in (2, 4):
+            p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+            kw = dict(frequency=2e38, masks=words, mask_index=np.zeros((2, n), np.int32))
+            if n == 2:
+                assert np.all(J.jet_generate_trace_rules(m, p, 2, n, tau, 3, **kw) == 17)
+            else:
+                with pytest.raises(J.JetError) as e:
+                    J.jet_generate_trace_rules(m, p, 2, n, tau, 3, **kw)
+                assert e.value.code == J.JET_E_DEVICE and "finite" in str(e.value)
+            J.jet_prefix_free(p)
+    finally:
+        J.jet_model_free(m)
