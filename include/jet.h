@@ -426,9 +426,9 @@ const char *jet_last_error(void);
  * overlap need workspaces of their own.
  * What the host can see (NULL, counts, types, alignment) is refused with
  * JET_E_INVALID before anything is enqueued. What lies in device memory cannot
- * be refused: kernels check it against the counts given here, and a sequence
- * or row that lies outside of them is left out: nothing is read or written
- * for it.
+ * be refused: kernels check it against the counts given here. A sequence that
+ * lies outside of them is left out (nothing is read or written for it), and a
+ * row's list (history, biases) whose offsets do is empty.
  * ---------------------------------------------------------------------------
  */
 
@@ -462,8 +462,10 @@ typedef struct {
  * share no block. The call's rows are the last ones of each sequence: rows
  * row_offsets[s] .. row_offsets[s + 1] - 1 are its last tokens (n of them:
  * positions len[s] - n .. len[s] - 1). Slots and offsets outside the cache, or
- * rows outside [0, n_rows), leave the sequence out; a row at a position below
- * 0 is left out. */
+ * rows outside [0, n_rows), leave the sequence out (one of no tokens may start
+ * at n_slots, behind the last block; a cache of no slots has no sequences). A
+ * row at a position below 0 belongs to no token: writes and reads leave it out,
+ * and in attention it sees none. */
 typedef struct {
   int32_t n_seq;      /* 0 .. 65535 */
   int32_t n_rows;     /* rows of the row arrays; 0 .. 2^30 */

@@ -27,8 +27,9 @@ __device__ __forceinline__ QSeq qseq(const QBatch &b, const QCache &c, int s) {
   const int end = uniform(b.rows ? b.rows[s + 1] : s + 1);
   q.n = end - q.row0;
   q.lo = q.hi = 0;
-  const bool ok = q.slot0 >= 0 && q.slot0 < c.S && (q.slot0 & ((1 << c.lb) - 1)) == 0 && q.row0 >= 0 && end >= q.row0 &&
-                  end <= b.n_rows && q.len >= 0 && q.len <= (1 << 30) && q.len <= c.S - q.slot0;
+  // (slot0 = S: a sequence without tokens behind the last block of a full cache)
+  const bool ok = c.S > 0 && q.slot0 >= 0 && q.slot0 <= c.S && (q.slot0 & ((1 << c.lb) - 1)) == 0 && q.row0 >= 0 &&
+                  end >= q.row0 && end <= b.n_rows && q.len >= 0 && q.len <= (1 << 30) && q.len <= c.S - q.slot0;
   if (!ok) {
     q.slot0 = 0;
     q.len = q.n = q.row0 = q.pos0 = 0;
