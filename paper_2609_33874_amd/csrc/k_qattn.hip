@@ -57,7 +57,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // those same keys: a transposition of bytes inside the lane makes the A
 // operand, dim HD/16 c + i in product i.
 template <typename T, typename O, int FMT, int HD, int QB>
-__global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit, int per) {
+__global__ __launch_bounds__(64 * kWaves, HD * QB == 256 ? 2 : 4) void qattn_split_kernel(QAttn a, int nsplit, int per) {
   constexpr int ND = HD / 16, NK = HD / 32, LD = HD + 4;
   typedef QTile<HD> Tile;
   __shared__ float s_o[kWaves][16 * QB][LD];
@@ -125,9 +125,12 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qat
 
     float m[QB], l[QB];
     f32x4 acc[QB][ND];
-    int M = 0;  // V exponent byte of the accumulators' unit
+    // V exponent byte of the accumulators' unit: M while every query sees all keys
+    // of a tile, the larger of M and its query's Mq in the tiles after those
+    int M = 0, Mq[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
+      Mq[qb] = 0;
       m[qb] = -INFINITY;
       l[qb] = 0.0f;
 #pragma unroll
@@ -160,14 +163,19 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qat
       __builtin_amdgcn_sched_barrier(0);
       load_k(cur, min(t + kWaves, t1 - 1));
       __builtin_amdgcn_sched_barrier(0);
-      const int Mn = max(M, max(v_top(ve0), v_top(ve1)));
-      const float vs[2] = {v_scale(ve0, Mn), v_scale(ve1, Mn)}, unit = v_scale(M, Mn);
-      M = Mn;
       const bool all_seen = k0 + kTile <= vis_min;
+      const int Mn = all_seen ? max(M, max(v_top(ve0), v_top(ve1))) : M;
       Frag<f16> pf[QB];
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        float z[2][4], mx = -INFINITY;
+        float z[2][4], mx = -INFINITY, vs[2] = {v_scale(ve0, Mn), v_scale(ve1, Mn)}, unit = v_scale(M, Mn);
+        if (!all_seen) {  // a block that a query sees nothing of must not move its unit
+          const int old = max(M, Mq[qb]);
+          Mq[qb] = max(old, max(k0 < vis[qb] ? v_top(ve0) : 0, k0 + 16 < vis[qb] ? v_top(ve1) : 0));
+          vs[0] = v_scale(ve0, Mq[qb]);
+          vs[1] = v_scale(ve1, Mq[qb]);
+          unit = v_scale(old, Mq[qb]);
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -187,7 +195,8 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qat
           for (int e = 0; e < 4; ++e) {
             p[kb][e] = __builtin_amdgcn_exp2f(z[kb][e] - ms15);  // 2^15 p, and l in that unit
             sum += p[kb][e];
-            // (a masked key's 0 must stay 0 where the block's scale is NaN)
+            // (a masked key's 0 must stay 0 where the block's scale is NaN, or
+            // larger than the unit)
             p[kb][e] = z[kb][e] == -INFINITY ? 0.0f : p[kb][e] * vs[kb];
           }
         l[qb] = l[qb] * alpha + sum;
@@ -200,6 +209,7 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qat
                                    f2h2(p[1][2], p[1][3]));
         pf[qb].v = __builtin_bit_cast(f16x8, u);
       }
+      M = Mn;
 #pragma unroll
       for (int w = 0; w < Tile::VW; ++w) {
         uint32_t a0[4] = {cur.v[0][w], cur.v[1][w], cur.v[2][w], cur.v[3][w]};
@@ -221,10 +231,10 @@ __global__ __launch_bounds__(64 * kWaves, HD == 256 || QB == 2 ? 2 : 4) void qat
 
     // the waves' results in LDS, in units of 1
     const int tid = here(threadIdx.x), go = tid >> 4 & 3, co = tid & 15;
-    const float up = pow2i(max(M - kExpBias - 15, -126));
     __syncthreads();  // the last block's have been read
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
+      const float up = pow2i(max(max(M, Mq[qb]) - kExpBias - 15, -126));
       float lt = l[qb] + __shfl_xor(l[qb], 16);
       lt += __shfl_xor(lt, 32);
       const int q = qb * 16 + co;

@@ -17,6 +17,7 @@
 // as 16-bit tiles of the same stream; there no split is made and every query
 // runs the same operations in the same order whatever block it lies in.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_core.h"
 #include "qattn.h"
@@ -212,7 +213,13 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) vis_min = min(vis_min, __shfl_xor(vis_min, o));
       const bool idle = sb + wave * QB * 16 >= slots;  // no query: loads and barriers only
-      int M = 0;  // V exponent byte of the accumulators' unit
+      // V exponent byte of the accumulators' unit: M, the largest of the blocks so
+      // far, while every query sees every block; where a query does not, 2^low less
+      // (0 in all tiles but a causal call's last ones). udown = 2^-low.
+      int M = 0;
+      float low[QB], udown[QB];
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) low[qb] = 0.0f, udown[qb] = 1.0f;
 
       int ec = re, stage = 0;  // the current tile's scale bytes
       __syncthreads();         // the block before is done with the stages
@@ -222,7 +229,10 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
       }
       Tile ahead = next_tile(cur);
       if (ahead.nk > 0 && ahead.cs < 0) load(ahead);
-      while (cur.nk > 0) {
+      // One tile. ALL: a whole one that every query of the workgroup sees all of
+      // (with the other tiles' cases in the same code those cost 2 to 4%).
+      auto step = [&](auto all) __attribute__((always_inline)) {
+        constexpr bool ALL = decltype(all)::value;
         if constexpr (OWN) wait_vmcnt<0>();  // (own tiles are loaded into LDS directly)
         __syncthreads();                     // this tile is in place, and every wave is done with the other stage
         const int ea = re;
@@ -263,7 +273,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
           };
           // fragments are read one group of products ahead, and no further (the
           // compiler would hold them all in registers)
-          if (cur.nk > 48) {
+          if (ALL || cur.nk > 48) {
             u32x4 f[2][4];
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) f[0][kb] = read_k(0, kb);
@@ -309,14 +319,16 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
           }
           const bool grown = Mn != M;
           const float unit = v_scale(M, Mn);
+          const int M0 = M;
           M = Mn;
-          const bool seen = pre && cur.t0 + KT <= min(vis_min, key1);  // every key of the tile by every query
+          const bool seen = ALL || (pre && cur.t0 + KT <= min(vis_min, key1));  // every key of the tile by every query
           Frag<f16> pf[QB][2];
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) {
             // z = s f, the largest z, and p = 2^(z - m): where all keys are
             // seen z itself is not needed (f >= 0: largest z from largest s)
-            float f[4], mx = -INFINITY;
+            float f[4], mx = -INFINITY, un = unit;
+            bool turn = false;
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) f[kb] = ks2[kb] * fq[qb];
             if (seen) {
@@ -338,24 +350,38 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
                 }
                 f[kb] = 1.0f;
               }
+              // blocks that the query sees nothing of must not move its unit (with
+              // own rows all see the same blocks)
+              if constexpr (!OWN) {
+                const int old = M0 - (int)low[qb];
+                int top = old;
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb)
+                  if (kb * 16 <= last) top = max(top, v_top(ve[kb]));
+                un = v_scale(old, top);
+                turn = top != old;
+                low[qb] = (float)(M - top);
+                udown[qb] = pow2i(max(top - M, -126));
+              }
             }
             mx = query_max(mx);
             // the accumulators are rescaled when some query's maximum lags too
             // far behind (or their unit grew), not whenever one moves; each query
             // by its own maximum alone, whatever the others in its wave do
             const bool lags = mx > m[qb] + kLag;
-            if (grown || __any(lags)) {
+            if (grown || __any(turn || lags)) {
               const float mn = lags ? mx : m[qb];
               const float al = lags ? __builtin_amdgcn_exp2f(m[qb] - mn) : 1.0f;
               m[qb] = mn;
               l[qb] *= al;
 #pragma unroll
-              for (int d = 0; d < ND; ++d) acc[qb][d] *= al * unit;
+              for (int d = 0; d < ND; ++d) acc[qb][d] *= al * un;
             }
-            const float ms = (m[qb] == -INFINITY ? 0.0f : m[qb]) - (float)kUnit;
+            const float m0 = m[qb] == -INFINITY ? 0.0f : m[qb];
             float p[4][4], sum = 0.0f;
             if (near) {
               // p' = 2^(z - m + log2 vs), and l adds it up in p's own unit
+              const float ms = m0 - ((ALL ? 0.0f : low[qb]) + (float)kUnit);
 #pragma unroll
               for (int kb = 0; kb < 4; ++kb) {
                 const float mk = ms - (float)(ve[kb] - Mn);
@@ -367,18 +393,21 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
                 }
                 sum = fmaf(part, pow2i(Mn - ve[kb]), sum);
               }
+              l[qb] = ALL ? l[qb] + sum : fmaf(sum, udown[qb], l[qb]);
             } else {
+              const float ms = m0 - (float)kUnit;
 #pragma unroll
               for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const float x = __builtin_amdgcn_exp2f(fmaf(s[qb][kb][e], f[kb], -ms));
                   sum += x;
-                  // (a masked key's 0 must stay 0 where the scale is NaN)
-                  p[kb][e] = !seen && s[qb][kb][e] == -INFINITY ? 0.0f : x * vs[kb];
+                  // (a masked key's 0 must stay 0 where the scale is NaN, or
+                  // larger than the unit)
+                  p[kb][e] = !seen && s[qb][kb][e] == -INFINITY ? 0.0f : x * v_scale(ve[kb], ALL ? M : M - (int)low[qb]);
                 }
+              l[qb] += sum;
             }
-            l[qb] += sum;
 #pragma unroll
             for (int mm = 0; mm < 2; ++mm) {
               const uint4 u = make_uint4(f2h2(p[2 * mm][0], p[2 * mm][1]), f2h2(p[2 * mm][2], p[2 * mm][3]),
@@ -389,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
           }
 #pragma unroll
           for (int mm = 0; mm < 2; ++mm) {
-            if (mm * 32 >= cur.nk) continue;
+            if (!ALL && mm * 32 >= cur.nk) continue;
             auto read_v = [&](int d, int half) {
               return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                   (lds_s16x4 *)(uintptr_t)((va ^ (d << 5)) + (mm * 32 + half * 16) * RB));
@@ -423,11 +452,15 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
         cur = ahead;
         ahead = after;
         stage ^= 1;
+      };
+      if constexpr (!OWN) {
+        const int seen_by_all = a.causal ? min(key1, pos0 + sb / G + 1) : key1;
+        while (cur.nk > 0 && cur.t0 + KT <= seen_by_all) step(std::true_type{});
       }
+      while (cur.nk > 0) step(std::false_type{});
 
       {
       const int lane = here(threadIdx.x) & 63, g = lane >> 4, l16 = lane & 15;
-      const float up = pow2i(max(M - kExpBias - kUnit, -126));
       const int64_t n = (int64_t)a.b.n_rows * a.Hq;
       const Parts parts = parts_of(a.ws, n, nsplit, HD);
 #pragma unroll
@@ -435,6 +468,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
         float lt = l[qb] + __shfl_xor(l[qb], 16);
         lt += __shfl_xor(lt, 32);
         lt *= pow2i(-kUnit);
+        const float up = pow2i(max(M - (int)low[qb] - kExpBias - kUnit, -126));
         const int s = sb + (wave * QB + qb) * 16 + l16, head = h * G + s % G;
         if (s >= slots) continue;
         const int64_t row = row0 + s / G, at = row * a.Hq + head;

@@ -6,10 +6,10 @@
 // sum of the softmax. The 8-bit values are exact in f16, so both products run
 // on the matrix cores in f16 with the scales outside of them: K's on the
 // scores, V's on the probabilities. A probability goes into the second product
-// as p 2^(ev - M) 2^u in f16, M the largest V exponent met so far (the
-// accumulators are in units of 2^(M - u) and rescaled when M grows), so that
-// what it loses is its rounding to 11 bits, or 2^-(25 + u) of the largest value
-// (u is 15, or 7 where p may reach 2^8).
+// as p 2^(ev - M) 2^u in f16, M the largest V exponent met so far in blocks of
+// which the query sees a token (the accumulators are in units of 2^(M - u) and
+// rescaled when M grows), so that what it loses is its rounding to 11 bits, or
+// 2^-(25 + u) of the largest value (u is 15, or 7 where p may reach 2^8).
 // bf16 queries enter as f16 times a power of two that puts a row's largest
 // value in [2^14, 2^15): exact down to 2^-30 of it.
 #pragma once

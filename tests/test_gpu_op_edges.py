@@ -5,8 +5,9 @@ import numpy as np
 import pytest
 import torch
 
+import _qcache_ref as ref
 from paper_2609_33874_amd import jet as J
-from test_gpu_ops import case, check_attention, i32, i64, offsets  # noqa: F401
+from test_gpu_ops import Pair, case, check_attention, i32, i64, offsets, values  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +65,44 @@ def test_an_empty_sequence_behind_a_full_cache(max_rows, max_len):
             J.jet_qcache_read(full, i64(slot0), i32(lens), k, v, row_offsets=i32(offsets(rows)))
             assert torch.all(k == 5.0) and torch.all(v == 5.0)
             assert all(torch.equal(a, b) for a, b in zip(before, full.tensors))
+
+
+def causal_check(p, q, rows, **kw):
+    """One sequence's last rows, each against its own tolerance: `big` is the largest |v| of the tokens that the row
+    sees, whatever later ones hold (test_gpu_ops.py says where the terms come from)."""
+    R, Hq, hd = q.shape
+    G, n = Hq // p.H, p.lens[0]
+    o = torch.empty((R, Hq, hd), device="cuda")
+    J.jet_qcache_attention(p.gpu, i64(p.slot0), i32(p.lens), q, o, row_offsets=i32([0, rows]), **kw)
+    got, qd, scale, u = o.double().cpu().numpy(), q.double().cpu().numpy(), hd ** -0.5, 2.0 ** -24
+    for h in range(p.H):
+        k, v = p.k[h].values(p.slot0[0], n), p.v[h].values(p.slot0[0], n)
+        hs = slice(h * G, h * G + G)
+        want, _, pv, qk = ref.attention(qd[:, hs], k, v, scale, n - rows, True)
+        ds = (hd + 6) * u * scale * qk[..., None]
+        big = np.array([np.abs(v[:n - rows + i + 1]).max() for i in range(rows)])[:, None, None]
+        tol = pv * (2 * np.expm1(np.minimum(ds, 1.0)) + (n + 64) * u + 2.0 ** -11) + n * 2.0 ** -32 * big * 2
+        tol = tol + np.abs(want) * 1.01 * u
+        err = np.abs(got[:, hs] - want)
+        assert np.all(err <= tol), (h, np.argwhere(err > tol)[:3], (err / tol).max())
+
+
+@pytest.mark.parametrize("hd,fmt", [(128, 0), (64, 1), (256, 0)])
+@pytest.mark.parametrize("rows,G,max_rows", [(3, 2, 3), (20, 1, 1), (6, 5, 6), (7, 7, 1), (40, 1, 40), (40, 5, 40),
+                                             (90, 4, 90), (150, 1, 1)])
+@pytest.mark.parametrize("max_len", [200, 6000])
+def test_rows_do_not_depend_on_values_after_them(rows, G, max_rows, max_len, hd, fmt):
+    """V of later tokens 2^45 and 2^90 larger: rows that do not see those keep their own values' precision. The steps
+    lie at block borders, in tiles that some queries see and others do not."""
+    rng = np.random.default_rng(52)
+    n = 274
+    p = Pair([n], 1, hd, 16, fmt)
+    k = torch.tensor(values(rng, (n, 1, hd), 0.1)).float().cuda()
+    v = torch.tensor(values(rng, (n, 1, hd), 0.1)).float().cuda()
+    first = ((n - rows) // 16 + 1) * 16
+    assert n - rows < first < n
+    for t in {first, max(first, (n - rows // 3) // 16 * 16)}:
+        v[t:] *= 2.0 ** 45
+    p.write([0], k, v, [n])
+    q = torch.tensor(values(rng, (rows, G, hd), 0.2)).half().cuda()
+    causal_check(p, q, rows, max_rows=max_rows, max_len=max_len)
