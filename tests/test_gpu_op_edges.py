@@ -106,3 +106,21 @@ def test_rows_do_not_depend_on_values_after_them(rows, G, max_rows, max_len, hd,
     p.write([0], k, v, [n])
     q = torch.tensor(values(rng, (rows, G, hd), 0.2)).half().cuda()
     causal_check(p, q, rows, max_rows=max_rows, max_len=max_len)
+
+
+@pytest.mark.parametrize("R,V,pad", [(2, 20000, 0), (1, 4097, 3)])
+def test_a_repeated_logit_is_divided(R, V, pad):
+    """z / repetition, rounded once: whatever its inverse rounds to, and where that is infinite."""
+    rng = np.random.default_rng(53)
+    z = rng.normal(size=(R, V)).astype(np.float32) * 10
+    z[:, :9] = [1e-44, -1e-44, 3e38, -3e38, np.inf, -np.inf, 1e-30, 0.0, 2.0 ** -126]
+    ids = np.tile(np.arange(V, dtype=np.int32), R)
+    for rep in (1.3, 3.0, 0.7, 1.0000001, 1e-40, 2.0 ** -149, 3e38, 1e30, 0.1):
+        r = np.full(R, rep, np.float32)
+        x = torch.empty((R, V + pad), device="cuda")[:, pad:]
+        x.copy_(torch.tensor(z))
+        got = J.jet_logits_adjust(x, history=(i32([i * V for i in range(R + 1)]), torch.tensor(ids).cuda()),
+                                  hist_prompt=i32([V] * R), repetition=torch.tensor(r).cuda()).cpu().numpy()
+        with np.errstate(over="ignore", under="ignore"):
+            want = np.where(z > 0, z / r[:, None], z * r[:, None])
+        np.testing.assert_array_equal(got, want)
