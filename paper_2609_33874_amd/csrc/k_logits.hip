@@ -119,9 +119,12 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
       if (mask && i + N <= nv) m[k] = mask[i >> 5] >> (i & 31);
     }
   }
-  const uint4 zero = {0, 0, 0, 0};
+  // no bias is -0.0: added to any logit it leaves that logit, -0.0 too
+  const uint32_t sign = __float_as_uint(-0.0f);
+  const uint4 zero = {0, 0, 0, 0}, no_bias = {sign, sign, sign, sign};
   if (hist || biased) {
-    for (int i = tid; i < kSlice / 4; i += kLogitThreads) reinterpret_cast<uint4 *>(cnt)[i] = zero;
+    const uint4 start = hist ? zero : no_bias;
+    for (int i = tid; i < kSlice / 4; i += kLogitThreads) reinterpret_cast<uint4 *>(cnt)[i] = start;
     __syncthreads();
   }
   if constexpr (HIST) {
@@ -151,10 +154,10 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
       if constexpr (VEC) {
         const uint4 q = hist ? *reinterpret_cast<const uint4 *>(&cnt[at(i)]) : zero;
         c[k] = q.x; c[k + 1] = q.y; c[k + 2] = q.z; c[k + 3] = q.w;
-        if (hist && biased) *reinterpret_cast<uint4 *>(&cnt[at(i)]) = zero;
+        if (hist && biased) *reinterpret_cast<uint4 *>(&cnt[at(i)]) = no_bias;
       } else {
         c[k] = hist ? cnt[at(i)] : 0u;
-        if (hist && biased) cnt[at(i)] = 0u;
+        if (hist && biased) cnt[at(i)] = sign;
       }
     }
     if (hist && biased) __syncthreads();
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
           uint32_t q = 0;
 #pragma unroll
           for (int e = 0; e < N; ++e) q = e == j ? count_of(k * N + e) : q;
-          const float b = biased ? bias[at(i + j)] : 0.0f;
+          const float b = biased ? bias[at(i + j)] : -0.0f;
           T x = in[i + j];
           if (q || b != 0.0f) x = from_f<T>(adjusted(to_f<T>(x), q, b, w));
           const bool allowed = !none && (!mask || (mask[(i + j) >> 5] >> ((i + j) & 31) & 1));
@@ -194,10 +197,13 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
         continue;
       }
       uint32_t seen = 0;
-      float b[N] = {};
+      float b[N];
       bool off = false;  // any bias
 #pragma unroll
-      for (int j = 0; j < N; ++j) seen |= count_of(k * N + j);
+      for (int j = 0; j < N; ++j) {
+        seen |= count_of(k * N + j);
+        b[j] = -0.0f;
+      }
 #pragma unroll
       for (int j = 0; j < N; j += 4) {
         if (biased) {
@@ -235,7 +241,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
       const int i = k * kLogitThreads + tid;
       if (i >= nv) break;
       const bool allowed = !none && (!mask || (mask[i >> 5] >> (i & 31) & 1));
-      const float b = biased ? bias[at(i)] : 0.0f;
+      const float b = biased ? bias[at(i)] : -0.0f;
       T x = in[i];
       if (count_of(k) || b != 0.0f) x = from_f<T>(adjusted(to_f<T>(x), count_of(k), b, w));
       out[i] = allowed ? x : from_f<T>(-INFINITY);

@@ -124,3 +124,29 @@ def test_a_repeated_logit_is_divided(R, V, pad):
         with np.errstate(over="ignore", under="ignore"):
             want = np.where(z > 0, z / r[:, None], z * r[:, None])
         np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_tokens_of_no_list_keep_their_bits(dtype, inplace):
+    """-0.0, a NaN's payload and the rest, beside tokens that have a history or a bias."""
+    V = 4096 + 40
+    bits = torch.int32 if dtype == torch.float32 else torch.int16
+    g = torch.Generator().manual_seed(54)
+    z = torch.randn((2, V), generator=g).to(dtype)
+    z[:, ::3] = -0.0
+    nan = {torch.float32: 0x7fc00123, torch.float16: 0x7e12, torch.bfloat16: 0x7fc5}[dtype]
+    z.view(bits)[:, 1::7] = nan
+    z = z.cuda()
+    was = z.clone()
+    listed = list(range(5, V, 16))
+    out = J.jet_logits_adjust(z, None if inplace else torch.empty_like(z),
+                              history=(i32([0, len(listed), len(listed)]), i32(listed)),
+                              frequency=torch.ones(2, device="cuda"),
+                              bias=(i32([0, 1, 1 + len(listed)]), i32([3] + [v + 1 for v in listed]),
+                                    torch.full((1 + len(listed),), 0.5, device="cuda")))
+    got, want = out.view(bits).cpu(), was.view(bits).cpu()
+    for r, touched in enumerate(({*listed, 3}, {v + 1 for v in listed})):
+        rest = [v for v in range(V) if v not in touched]
+        assert torch.equal(got[r, rest], want[r, rest])
+        assert not torch.equal(got[r], want[r])
