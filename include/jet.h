@@ -218,7 +218,8 @@ typedef struct {
   const uint32_t *masks;          /* uint32[n_masks][ceil(vocab / 32)] or NULL: bit v % 32 of
                                      word v / 32 allows token v; each allows some token */
   const int32_t *mask_index;      /* int32[n_q][n_steps]: the step's mask, < 0: any token.
-                                     Needed when masks are given */
+                                     Needed when masks are given; one that names no mask
+                                     is refused, without masks too */
 } jet_trace_rules;
 
 /*

@@ -134,9 +134,9 @@ Status check_rules(const jet_trace_rules *r, int32_t n_q, int32_t n_steps, int64
       }
       if (!any) return bad("mask " + std::to_string(m) + " allows no token");
     }
-    for (int64_t i = 0; i < (int64_t)n_q * n_steps; ++i)
-      if (r->mask_index[i] >= r->n_masks) return bad("mask_index " + std::to_string(i) + " names no mask");
   }
+  for (int64_t i = 0; r->mask_index && i < (int64_t)n_q * n_steps; ++i)
+    if (r->mask_index[i] >= r->n_masks) return bad("mask_index " + std::to_string(i) + " names no mask");
   return Status::ok();
 }
 

@@ -238,8 +238,8 @@ def jet_generate_trace_rules(model, prefix, n_q: int, n_steps: int, temperature:
         words = (jet_model_info(model)["vocab"] + 31) // 32
         r.n_masks = masks.shape[0]
         r.masks = host(masks, np.uint32, r.n_masks * words)
-        if mask_index is not None:
-            r.mask_index = host(mask_index, np.int32, n_q * max(int(n_steps), 0))
+    if mask_index is not None:
+        r.mask_index = host(mask_index, np.int32, n_q * max(int(n_steps), 0))
     _check(lib().jet_generate_trace_rules(model, prefix, int(n_steps), float(temperature),
                                           ctypes.c_uint64(seed & 0xFFFFFFFFFFFFFFFF), ctypes.byref(r), ot))
     return out

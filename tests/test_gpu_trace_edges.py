@@ -62,3 +62,25 @@ def test_a_forbidden_token_is_never_sampled(flags, tau, model_dir):
             J.jet_prefix_free(p)
     finally:
         J.jet_model_free(m)
+
+
+def test_mask_indices_without_masks(model_dir):
+    """Steps that name a mask are refused where there is none; steps that name none run as without rules."""
+    path = jet_synth.ensure_model("small_gqa_bf16", cache_dir=model_dir)
+    wl = jet_synth.make_workload("small", n_questions=2)
+    none = np.zeros((0, (3000 + 31) // 32), np.uint32)
+    m = J.jet_model_load(path, dtype=J.JET_F16)
+    try:
+        p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+        for masks in (None, none):
+            for index in (np.zeros((2, 3), np.int32), np.array([[-1, -1, -1], [-1, -1, 0]], np.int32)):
+                with pytest.raises(J.JetError) as e:
+                    J.jet_generate_trace_rules(m, p, 2, 3, 0.0, 0, masks=masks, mask_index=index)
+                assert e.value.code == J.JET_E_INVALID and "mask" in str(e.value)
+        got = J.jet_generate_trace_rules(m, p, 2, 3, 0.0, 0, mask_index=np.full((2, 3), -1, np.int32))
+        J.jet_prefix_free(p)
+        p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+        np.testing.assert_array_equal(got, J.jet_generate_trace(m, p, 2, 3))
+        J.jet_prefix_free(p)
+    finally:
+        J.jet_model_free(m)
