@@ -576,7 +576,7 @@ typedef struct {
   const int32_t *mask_index;      /* device, [n_rows]: the row's mask, or < 0:
                                      all allowed; NULL: mask r for row r
                                      (n_masks >= n_rows). An index >= n_masks
-                                     allows nothing. */
+                                     allows nothing, without masks too. */
 } jet_logits_args;
 int jet_logits_adjust(const jet_logits_args *args, void *hip_stream);
 

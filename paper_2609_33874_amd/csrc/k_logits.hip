@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits_adjust_kernel(LogitsArgs
   const RowRules w = {*rp, *sp, *fp};
   if (h0 < 0 || h1 < h0 || h1 > a.n_hist) h0 = h1 = 0;
   if (b0 < 0 || b1 < b0 || b1 > a.n_bias) b0 = b1 = 0;
-  const int mi = !a.masks ? -1 : a.mask_index ? index : r;
+  const int mi = a.mask_index ? index : a.masks ? r : -1;  // (without masks n_masks is 0)
   const bool none = mi >= a.n_masks;  // a mask that does not exist allows nothing
   const uint32_t *mask = mi < 0 || none ? nullptr : a.masks + (int64_t)mi * a.mask_ld + v0 / 32;
   const bool hist = HIST && h1 > h0, biased = BIAS && b1 > b0;

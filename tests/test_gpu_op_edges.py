@@ -150,3 +150,12 @@ def test_tokens_of_no_list_keep_their_bits(dtype, inplace):
         rest = [v for v in range(V) if v not in touched]
         assert torch.equal(got[r, rest], want[r, rest])
         assert not torch.equal(got[r], want[r])
+
+
+@pytest.mark.parametrize("R,V", [(3, 50), (65600, 50), (40, 4096), (3, 151936)])
+def test_mask_indices_without_masks(R, V):
+    """Every index >= 0 names no mask and allows nothing, < 0 allows all."""
+    z = torch.randn((R, V), device="cuda")
+    idx = (torch.arange(R, device="cuda") % 3 - 1).to(torch.int32)
+    out = J.jet_logits_adjust(z, torch.empty_like(z), mask_index=idx)
+    assert torch.equal(out, torch.where(idx[:, None] < 0, z, -np.inf))
