@@ -192,7 +192,8 @@ int jet_prefill_prefix(jet_model *model, int32_t n_q, const int64_t *prefix_offs
  *   seed: any 64-bit value.
  *   out_tokens: host or device, int32[n_q * n_steps] (question-major), may be
  *     NULL.
- * Limits: n_steps < 2^20, n_q < 2^26, vocab <= 2^18; P_q + n_steps <= max_ctx.
+ * Limits: n_steps < 2^20, n_q < 2^26, n_q n_steps <= 2^30, vocab <= 2^18;
+ *   P_q + n_steps <= max_ctx.
  * Errors: JET_E_INVALID (arguments, a prefix of another model; the prefix is
  *   unchanged), JET_E_CAPACITY (max_ctx; unchanged), JET_E_OOM (before any
  *   change: unchanged), JET_E_DEVICE (the prefix is then in an unspecified
@@ -211,7 +212,8 @@ typedef struct {
   float presence, frequency;  /* finite; 0: no penalty */
   int32_t n_masks;
   const int64_t *context_offsets; /* int64[n_q + 1] or NULL */
-  const int32_t *context_tokens;  /* int32[context_offsets[n_q]], e.g. the prefixes */
+  const int32_t *context_tokens;  /* int32[context_offsets[n_q]], e.g. the prefixes; n_q
+                                     times (the longest context + n_steps) <= 2^30 */
   const int64_t *bias_offsets;    /* int64[n_q + 1] or NULL */
   const int32_t *bias_tokens;     /* token ids, and what is added to their logits (finite) */
   const float *bias_values;

@@ -1,6 +1,7 @@
 // Checks of the operators' arguments that need no GPU.
 #include "op_checks.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace jet {
@@ -110,6 +111,10 @@ Status check_rules(const jet_trace_rules *r, int32_t n_q, int32_t n_steps, int64
     if (r->context_offsets[n_q] > INT32_MAX) return bad("too many context tokens");
     s = check_ids_host(r->context_tokens, r->context_offsets[n_q], vocab, "context_tokens");
     if (!s) return s;
+    int64_t longest = 0;  // (every question has a row of so many tokens)
+    for (int32_t q = 0; q < n_q; ++q) longest = std::max(longest, r->context_offsets[q + 1] - r->context_offsets[q]);
+    if (n_q * (longest + n_steps) > kMaxTraceTokens)
+      return bad("n_q times the longest context and n_steps exceeds 2^30");
   }
   if (r->bias_offsets) {
     s = check_offsets(r->bias_offsets, n_q, 0, "bias_offsets");

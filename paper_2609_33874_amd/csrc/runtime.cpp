@@ -1406,6 +1406,7 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   for (int32_t q = 0; q < nq; ++q)
     if (offs[q + 1] - offs[q] + n > m->max_ctx)
       return Status::err(JET_E_CAPACITY, "prefix " + std::to_string(q) + " plus the trace is longer than max_ctx");
+  if ((int64_t)nq * n > kMaxTraceTokens) return Status::err(JET_E_INVALID, "n_q times n_steps exceeds 2^30");
   TRY(check_rules(rules, nq, n, h.vocab));
   if (n == 0) return Status::ok();
   const bool out_dev = out && is_device_ptr(out), qc = m->qfmt >= 0;
@@ -1446,7 +1447,6 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   if (rules && rules->context_offsets)
     for (int32_t q = 0; q < nq; ++q) ctx = std::max(ctx, rules->context_offsets[q + 1] - rules->context_offsets[q]);
   const int64_t ldt = ctx + n;
-  if (R * ldt > (1 << 30)) return Status::err(JET_E_INVALID, "context and trace tokens exceed 2^30");
   int32_t *d_hist;
   TRY(ws_t<int32_t>(m, "gen_tok", (size_t)(R * ldt), &d_hist));
   d_tok = d_hist + ctx;

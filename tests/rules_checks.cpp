@@ -47,8 +47,26 @@ static void check_mask_indices() {
   CHECK(refused(r, 2, 3));
 }
 
+// Contexts are held in rows as long as the longest: refused before anything is
+// allocated for them.
+static void check_context_sizes() {
+  const int32_t n_q = 1025;
+  std::vector<int32_t> tokens((1 << 20) - 1, 3);
+  std::vector<int64_t> offsets(n_q + 1, (int64_t)tokens.size());
+  offsets[0] = 0;
+  jet_trace_rules r = plain();
+  r.context_offsets = offsets.data();
+  r.context_tokens = tokens.data();
+  CHECK(refused(r, n_q, 1));       // 1025 2^20
+  CHECK(!refused(r, n_q - 1, 1));  // 2^30
+  CHECK(refused(r, n_q - 1, 2));
+  for (int64_t &o : offsets) o = o < 1000 ? o : 1000;
+  CHECK(!refused(r, n_q, 1));
+}
+
 int main() {
   check_mask_indices();
+  check_context_sizes();
   std::printf("%d failure(s)\n", g_fail);
   return g_fail != 0;
 }

@@ -84,3 +84,28 @@ def test_mask_indices_without_masks(model_dir):
         J.jet_prefix_free(p)
     finally:
         J.jet_model_free(m)
+
+
+@pytest.mark.parametrize("flags", [0, J.JET_FLAG_QCACHE_INT8])
+def test_a_refused_context_leaves_no_memory_behind(flags, model_dir):
+    import torch
+    path = jet_synth.ensure_model("small_gqa_bf16", cache_dir=model_dir)
+    n_q = 1025
+    wl = jet_synth.from_lists([np.array([q % 3000], np.int32) for q in range(n_q)],
+                              [[np.array([1], np.int32)] for _ in range(n_q)])
+    off = np.full(n_q + 1, (1 << 20) - 1, np.int64)
+    off[0] = 0
+    m = J.jet_model_load(path, dtype=J.JET_F16, flags=flags)
+    try:
+        p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+        free = []
+        for _ in range(4):
+            with pytest.raises(J.JetError) as e:
+                J.jet_generate_trace_rules(m, p, n_q, 1, context=(off, np.zeros(off[-1], np.int32)))
+            assert e.value.code == J.JET_E_INVALID
+            torch.cuda.synchronize()
+            free.append(torch.cuda.mem_get_info()[0])
+        assert len(set(free)) == 1, free
+        J.jet_prefix_free(p)
+    finally:
+        J.jet_model_free(m)
