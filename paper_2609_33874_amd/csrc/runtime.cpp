@@ -1175,6 +1175,18 @@ Status palloc(jet_prefix *p, size_t bytes, void **out) {
   return Status::ok();
 }
 
+// A buffer of the prefix goes back to the model's pool (later work on the
+// stream that reuses it runs after what is queued there).
+void pfree(jet_prefix *p, void *buf) {
+  for (size_t i = 0; i < p->allocs.size(); ++i)
+    if (p->allocs[i].first == buf) {
+      p->m->pool.push_back({p->allocs[i].second, buf});
+      p->bytes -= p->allocs[i].second;
+      p->allocs.erase(p->allocs.begin() + (std::ptrdiff_t)i);
+      return;
+    }
+}
+
 // K and V buffers of an attention layer (and their scale bytes, in 8 bits).
 Status palloc_kv(jet_model *m, jet_prefix *p, int64_t l, size_t bytes) {
   TRY(palloc(p, bytes, &p->kcache[(size_t)l]));
@@ -1428,6 +1440,13 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
   const size_t new_kv = qc ? (size_t)(h.n_kv_heads * qslot2.back() * h.head_dim) : (size_t)(nblk * T2 * row_bytes);
   const size_t new_exp = (size_t)(h.n_kv_heads * (qslot2.back() / kQBlock));
   std::vector<void *> fresh;  // new K then V cache of each attention layer (and their scale bytes)
+  struct Unused {             // given back where the call ends before the prefix changes
+    jet_prefix *p;
+    std::vector<void *> &bufs;
+    ~Unused() {
+      for (void *b : bufs) pfree(p, b);
+    }
+  } unused{p, fresh};
   for (int64_t l = 0; l < h.n_layers; ++l) {
     if (m->layers[(size_t)l].gdn) continue;
     for (int kv = 0; kv < (qc ? 4 : 2); ++kv) {
@@ -1544,32 +1563,26 @@ Status generate(jet_model *m, jet_prefix *p, int32_t n, float tau, uint64_t seed
     TRY(upload(m, "gen_qlen", len, &d_qlen));
   }
   // attention caches laid out again with n free rows after each question
+  std::vector<void *> next;
+  next.swap(fresh);
   size_t fi = 0;
   for (int64_t l = 0; l < h.n_layers; ++l) {
     if (m->layers[(size_t)l].gdn) continue;
     if (qc) {
       KTimer t(m, JET_K_OTHER, 0, 0);
-      const jetk::QCache to = qcache_view(m, fresh[fi], fresh[fi + 1], (uint8_t *)fresh[fi + 2], (uint8_t *)fresh[fi + 3],
+      const jetk::QCache to = qcache_view(m, next[fi], next[fi + 1], (uint8_t *)next[fi + 2], (uint8_t *)next[fi + 3],
                                           qslot2.back());
       LAUNCH(jetk::launch_qcache_copy(qcache_of(m, p, l), to, d_qs_old, d_qs_new, d_qlen, nq, m->st));
     }
     for (int kv = 0; kv < (qc ? 4 : 2); ++kv) {
       void *buf = kv == 0 ? p->kcache[(size_t)l] : kv == 1 ? p->vcache[(size_t)l]
                 : kv == 2 ? (void *)p->kexp[(size_t)l] : (void *)p->vexp[(size_t)l];
-      void *nb = fresh[fi++];
+      void *nb = next[fi++];
       if (!qc) {
         KTimer t(m, JET_K_OTHER, 0, 0);
         LAUNCH(jetk::launch_kv_relayout(buf, nb, d_offs, nq, (int)nblk, T, T2, row_bytes, n, m->st));
       }
-      // the old buffer goes back to the model's pool (later work on the
-      // stream that reuses it runs after the copy)
-      for (size_t i = 0; i < p->allocs.size(); ++i)
-        if (p->allocs[i].first == buf) {
-          m->pool.push_back({p->allocs[i].second, buf});
-          p->bytes -= p->allocs[i].second;
-          p->allocs.erase(p->allocs.begin() + (std::ptrdiff_t)i);
-          break;
-        }
+      pfree(p, buf);
       if (kv == 0) p->kcache[(size_t)l] = nb;
       else if (kv == 1) p->vcache[(size_t)l] = nb;
       else if (kv == 2) p->kexp[(size_t)l] = (uint8_t *)nb;

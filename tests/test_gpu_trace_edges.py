@@ -109,3 +109,46 @@ def test_a_refused_context_leaves_no_memory_behind(flags, model_dir):
         J.jet_prefix_free(p)
     finally:
         J.jet_model_free(m)
+
+
+@pytest.mark.parametrize("flags", [0, J.JET_FLAG_QCACHE_INT8])
+def test_a_trace_too_long_for_the_memory_leaves_room_for_a_shorter_one(flags, model_dir):
+    """JET_E_OOM changes nothing: what had been allocated until then is given back."""
+    path = jet_synth.ensure_model("small_gqa_bf16", cache_dir=model_dir)
+    wl = jet_synth.make_workload("small", n_questions=8)
+    short = 2 ** 21 // (8 * 2 * 128 * (1 if flags else 2))  # four buffers of 2 MiB; of a long one the first fits there
+    args = (wl.q_cand_offsets, wl.cand_tok_offsets, wl.cand_tokens)
+
+    def load(budget):
+        m = J.jet_model_load(path, dtype=J.JET_F16, flags=flags, max_device_bytes=budget)
+        p = J.jet_prefill_prefix(m, wl.prefix_offsets, wl.prefix_tokens)
+        J.jet_score_candidates(m, p, *args)
+        return m, p
+
+    # the least budget under which the short trace runs, to 1 MiB
+    lo, hi = 0, 256
+    while hi - lo > 1:
+        mid = (lo + hi) // 2
+        try:
+            m, p = load(mid << 20)
+        except J.JetError:
+            lo = mid
+            continue
+        try:
+            J.jet_generate_trace(m, p, 8, short)
+            hi = mid
+        except J.JetError as e:
+            assert e.code == J.JET_E_OOM
+            lo = mid
+        J.jet_prefix_free(p)
+        J.jet_model_free(m)
+    m, p = load(hi << 20)
+    tok, _ = J.jet_score_candidates(m, p, *args)
+    for _ in range(2):
+        with pytest.raises(J.JetError) as e:
+            J.jet_generate_trace(m, p, 8, 3 * short)
+        assert e.value.code == J.JET_E_OOM
+    np.testing.assert_array_equal(J.jet_score_candidates(m, p, *args)[0], tok)
+    J.jet_generate_trace(m, p, 8, short)
+    J.jet_prefix_free(p)
+    J.jet_model_free(m)
