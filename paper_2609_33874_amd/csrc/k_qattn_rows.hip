@@ -454,7 +454,8 @@ __global__ __launch_bounds__(64 * NW, HD == 256 && NW == 4 ? 1 : 2) void qattn_r
         stage ^= 1;
       };
       if constexpr (!OWN) {
-        const int seen_by_all = a.causal ? min(key1, pos0 + sb / G + 1) : key1;
+        const int pos = pos0 + sb / G;  // of the block's first row
+        const int seen_by_all = pos < 0 ? 0 : a.causal ? min(key1, pos + 1) : key1;
         while (cur.nk > 0 && cur.t0 + KT <= seen_by_all) step(std::true_type{});
       }
       while (cur.nk > 0) step(std::false_type{});

@@ -159,3 +159,49 @@ def test_mask_indices_without_masks(R, V):
     idx = (torch.arange(R, device="cuda") % 3 - 1).to(torch.int32)
     out = J.jet_logits_adjust(z, torch.empty_like(z), mask_index=idx)
     assert torch.equal(out, torch.where(idx[:, None] < 0, z, -np.inf))
+
+
+LENS = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 500, 1031]
+
+
+@pytest.mark.parametrize("max_len", [1031, 20000])
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("hd,G,rows,qtype", [
+    (128, 6, 1, "f16"), (128, 1, 16, "bf16"), (128, 8, 2, "bf16"), (64, 4, 1, "f16"), (64, 8, 2, "bf16"),
+    (256, 4, 1, "bf16"), (256, 8, 2, "f16"), (256, 3, 8, "bf16"),
+    # 17 to 32 query slots: two blocks of 16 against one tile of keys (not for head_dim 256)
+    (128, 24, 1, "f16"), (128, 5, 4, "bf16"), (128, 32, 1, "bf16"), (64, 17, 1, "f16"), (64, 8, 4, "f16"),
+    (64, 2, 15, "bf16"), (256, 32, 1, "f16")])
+def test_few_query_slots(fmt, hd, G, rows, qtype, max_len):
+    """The kernel of up to 32 slots is chosen by max_rows; with a larger max_len its keys are split and joined."""
+    p, q = case(55, fmt, 16 << hd // 128, hd, 2, G, LENS, [rows] * len(LENS), qtype)
+    check_attention(p, q, [rows] * len(LENS), True, max_rows=rows, max_len=max_len)
+    check_attention(p, q, [rows] * len(LENS), False, out="f32", max_rows=rows, max_len=max_len)
+
+
+@pytest.mark.parametrize("max_len", [1031, 20000])
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("hd,G,rows,qtype", [
+    # 33 to 64 slots, 65 to 255, 256 and more: blocks of 64, 128 and 256 (64 and 128 for head_dim 256, 64 and 128 for 64)
+    (128, 33, 1, "f16"), (128, 8, 8, "bf16"), (128, 5, 9, "f16"), (128, 16, 5, "bf16"), (128, 1, 129, "f16"),
+    (128, 8, 32, "f16"), (128, 4, 70, "bf16"), (64, 64, 1, "bf16"), (64, 8, 8, "f16"), (64, 5, 20, "bf16"),
+    (64, 4, 70, "f16"), (256, 12, 4, "f16"), (256, 2, 60, "bf16"), (256, 4, 33, "f16")])
+def test_many_query_slots(fmt, hd, G, rows, qtype, max_len):
+    p, q = case(56, fmt, 16 << hd // 128, hd, 1, G, LENS, [rows] * len(LENS), qtype)
+    check_attention(p, q, [rows] * len(LENS), True, max_rows=rows, max_len=max_len)
+    check_attention(p, q, [rows] * len(LENS), False, out="f32", max_rows=rows, max_len=max_len)
+
+
+@pytest.mark.parametrize("max_rows,max_len", [(1, 100), (1, 20000), (12, 100), (12, 20000), (20, 100), (20, 20000),
+                                              (40, 100), (40, 20000), (100, 20000)])
+def test_sequences_outside_leave_their_rows_alone(max_rows, max_len):
+    """In the kernels of few and of many slots, split or not: outputs and lse of sequences that do not fit stay."""
+    p, _ = case(57, 0, 16, 128, 1, 3, [40] * 5, [2] * 5, "f16")
+    S = p.slots
+    slot0, lens = i64([-16, 8, S, S - 16, 0, 0, 2 ** 40]), i32([40, 40, 1, 17, -5, 2 ** 30 + 1, 1])
+    q = torch.ones((14, 3, 128), device="cuda", dtype=torch.float16)
+    for off in (range(0, 15, 2), [0, 2, 4, 6, 8, 10, 12, 15], [-1, 2, 1, 15, 14, 99, -3, 0]):
+        o, lse = torch.full_like(q, 5.0), torch.full((14, 3), 5.0, device="cuda")
+        J.jet_qcache_attention(p.gpu, slot0, lens, q, o, row_offsets=i32(off), max_rows=max_rows, max_len=max_len,
+                               lse=lse)
+        assert torch.all(o == 5.0) and torch.all(lse == 5.0)
