@@ -84,7 +84,8 @@ enum {
    * JET_FP32 modes, head_dim 64 or 128): a prefill attends to its own keys as
    * they are and then keeps them as a jet_qcache does (blocks of 32 tokens);
    * scoring and traces read them there, candidates' own keys stay in the mode's
-   * type. Half a JET_F16 prefix's bytes. In JET_FP32 the caches are read back
+   * type. Half a JET_F16 prefix's bytes; attention takes less time in a trace's
+   * steps and somewhat more in scoring. In JET_FP32 the caches are read back
    * into 32-bit rows for each call (validation). */
   JET_FLAG_QCACHE_INT8 = 4,
   JET_FLAG_QCACHE_E4M3 = 8
@@ -208,7 +209,7 @@ int jet_generate_trace(jet_model *model, jet_prefix *prefix, int32_t n_steps, fl
  * without context_offsets) and its t tokens so far; presence and frequency
  * count the latter alone. */
 typedef struct {
-  float repetition;           /* > 0; 1: no penalty */
+  float repetition;           /* > 0, and 1 / repetition finite; 1: no penalty */
   float presence, frequency;  /* finite; 0: no penalty */
   int32_t n_masks;
   const int64_t *context_offsets; /* int64[n_q + 1] or NULL */
@@ -533,7 +534,10 @@ int jet_qcache_read(const jet_qcache *cache, const jet_qcache_batch *batch, cons
  *     jet_qcache_attention_workspace gives for this batch (which may be 0,
  *     then NULL is fine). Nothing is kept in it between calls.
  * Scores, maxima, sums and outputs are held in 32 bits; probabilities are
- * rounded to f16 for the product with V.
+ * rounded to f16 for the product with V, in units of the largest scale of V
+ * blocks that the row has seen: an output is off by up to 2^-11 of the sum of
+ * p |v|, and 2^-32 of the largest |v| that the row sees for every such token,
+ * with an out of JET_T_F32 too.
  * Errors: JET_E_INVALID, JET_E_DEVICE.
  */
 int jet_qcache_attention(const jet_qcache *cache, const jet_qcache_batch *batch, int32_t n_q_heads, float scale,

@@ -8,7 +8,7 @@
 // without: every logit read and written once, the mask's bit and the history's
 // ids besides; each slice reads the row's whole history (from L2 after the first).
 // 256 rows of 151936 bf16 logits, histories of 200 .. 4096, 300 biases a row and
-// masks: 49 us (3.3 TB/s) where a copy of the logits takes 31, the mask alone 30:
+// masks: 51 us (3.1 TB/s) where a copy of the logits takes 31, the mask alone 30:
 // the counting and the listed tokens are some 500 vector instructions a wave, in
 // turn with the loads. Slices of 4096 because the work
 // that every slice repeats (clearing, the lists) and the waves that wait at its
@@ -29,8 +29,8 @@ constexpr int kSlice = 4096, kLogitThreads = 256;
 // the prompt. Without branches: where a vector has any token of the lists, its
 // tokens go through (a branch of each lane was slower), but for those that are of
 // no list in any lane; those of no list come out as they went in. A product with
-// 1 / repetition would save 2 of the 46 us that 256 rows take, but it rounds
-// twice, and overflows where the quotient need not.
+// 1 / repetition would save 4% of the time of 256 rows, but it rounds twice, and
+// overflows where the quotient need not.
 struct RowRules {
   float rep, pres, freq;
 };

@@ -370,10 +370,12 @@ __global__ __launch_bounds__(64 * W * NH) void qattn_join_kernel(QAttn a, int ns
 // splits, 584 in 16, 569 in 24; but 64 of 1024 .. 4096 keys 73 us in one, 81 in
 // four.
 // Many slots: a row's keys in equal parts, so many that they take the fewest
-// rounds of 512 workgroups over the keys of one, each workgroup counted as 512
-// keys longer than it is (its queries, its results and their joining): 320
-// workgroups of 4096 .. 8192 keys take 289 us in 2 splits (640: two rounds, the
-// second nearly empty), 220 in 3.
+// rounds of 512 workgroups (of 256 where only one fits on a CU) over the keys of
+// one, each workgroup counted as 512 keys longer than it is (its queries, its
+// results and their joining): 4 x 256 rows of 40 heads over 4096 .. 8192 keys, 160
+// workgroups of eight waves a split, take 302 us in one, 248 in 2 (two rounds, the
+// second a quarter full), 203 in 3, 225 in 4; 16 x 64 slots over 8192 keys, 128
+// workgroups of four waves, 113 in 2, 100 in 3, 82 in 4, 103 in 5.
 constexpr int64_t kFewSlots = 32, kLeastKeys = 512, kMostKeys = 6144, kFill = 512;
 struct Plan {
   bool few;

@@ -519,8 +519,10 @@ def jet_qcache_attention(cache: QCache, slot0, length, q, out, row_offsets=None,
     each sequence; lse: float32 [rows, n_q_heads] or None. scale: 1 /
     sqrt(head_dim) by default. max_rows, max_len: most rows and tokens of one
     sequence, by which the kernel and its launch are chosen (None: all rows, one
-    where there are no row_offsets, and all slots). workspace: a uint8 tensor of at least
-    jet_qcache_attention_workspace bytes (None: one is allocated). Returns out."""
+    where there are no row_offsets, and all slots: right, but slower where the
+    sequences are many or much shorter than that). workspace: a uint8 tensor of
+    at least jet_qcache_attention_workspace bytes for the same bounds (None: one
+    is allocated, for the stream that the work runs on). Returns out."""
     c, dev, L, torch = cache.c, cache.device, lib(), _t()[0]
     hd, shape = c.head_dim, q.shape
     if len(shape) != 3 or out.shape != shape:
